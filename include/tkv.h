@@ -429,6 +429,47 @@ int32_t tkv_sparse_append_dynamic(const tkv_sparse_desc* desc, tkv_sparse_cache*
                                   int32_t n_new, const int32_t* n_valid_host, void* stream);
 
 /* ---------------------------------------------------------------------------------
+ * A prompt's way into the caches
+ * ------------------------------------------------------------------------------- */
+
+/* Element types of the entry points that take more than fp16. */
+typedef enum { TKV_F16 = 0, TKV_BF16 = 1 } tkv_dtype;
+
+typedef struct {
+  uint32_t struct_size; /* sizeof(tkv_rope_desc)                                          */
+  int32_t n_q_heads;    /* any numbers from 1 to 1024                                     */
+  int32_t n_kv_heads;
+  int32_t head_dim;     /* 128                                                            */
+  int32_t in_dtype;     /* tkv_dtype of q, k, v and the weights                           */
+  int32_t out_dtype;    /* tkv_dtype of the outputs                                       */
+  int32_t norm;         /* 1: rows of q and k are normed; 0: not                          */
+  float eps;            /* >= 0                                                           */
+  int32_t rotary_dim;   /* R: the first R channels turn; a multiple of 16 up to 128, 0: none */
+  int32_t interleaved;  /* 0: channels i and i + R/2 are a pair; 1: channels 2i and 2i + 1 */
+  int64_t q_stride[2];  /* strides of tokens and heads in elements, multiples of 8; the   */
+  int64_t k_stride[2];  /* 128 channels of a row lie side by side                         */
+  int64_t v_stride[2];  /* (not read without v)                                           */
+} tkv_rope_desc;
+
+/*
+ * The rows that the caches and the attention calls take, from those of a model's projections, in one
+ * pass: every row (a head of a token) of q and k is normed,
+ *     y_c = x_c w_c / sqrt(mean over the 128 channels of x^2 + eps),
+ * and its first R channels are turned by the token's position: the pair (a, b) of frequency i < R/2 becomes
+ *     a cos t - b sin t, b cos t + a sin t,   t = positions[token] * inv_freq[i]
+ * (t is not rounded to 32 bits; everything else is float32, rounded once to the output's type).  v, where given, is
+ * converted and laid out only.
+ * q [n_tokens][Hq][128], k, v [n_tokens][Hkv][128] with the descriptor's strides, so that they may be slices of one fused
+ * projection; positions int32 [n_tokens] (any sign), inv_freq float32 [R/2], q_weight, k_weight [128] in in_dtype or NULL
+ * (ones): all device pointers.  q_out [n_tokens][Hq][128], k_out, v_out [n_tokens][Hkv][128] contiguous; an output may be its own
+ * input where both have the same type and layout.  Addresses of rows, weights and outputs are multiples of 16 bytes.  v and v_out: both or neither.
+ * n_tokens == 0 is a no-op that looks at the descriptor alone.
+ */
+int32_t tkv_qk_norm_rope(const tkv_rope_desc* desc, int32_t n_tokens, const void* q, const void* k, const void* v,
+                         const int32_t* positions, const float* inv_freq, const void* q_weight, const void* k_weight,
+                         void* q_out, void* k_out, void* v_out, void* stream);
+
+/* ---------------------------------------------------------------------------------
  * Offline identification (Sec. 4.1): which layers are quantization-friendly
  * ------------------------------------------------------------------------------- */
 

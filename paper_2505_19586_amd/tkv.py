@@ -58,6 +58,13 @@ class SparseStage1(C.Structure):
     _fields_ = [("k_absmax", C.c_void_p), ("keys_cm", C.c_void_p)]
 
 
+class RopeDesc(C.Structure):
+    _fields_ = [("struct_size", C.c_uint32), ("n_q_heads", C.c_int32), ("n_kv_heads", C.c_int32),
+                ("head_dim", C.c_int32), ("in_dtype", C.c_int32), ("out_dtype", C.c_int32), ("norm", C.c_int32),
+                ("eps", C.c_float), ("rotary_dim", C.c_int32), ("interleaved", C.c_int32),
+                ("q_stride", C.c_int64 * 2), ("k_stride", C.c_int64 * 2), ("v_stride", C.c_int64 * 2)]
+
+
 def lib() -> C.CDLL:
     """Loads libtkv.so (built by paper_2505_19586_amd/build.py); raises if absent."""
     global _LIB
@@ -106,6 +113,7 @@ def lib() -> C.CDLL:
         L.tkv_dense_preference_sizes.argtypes = [C.POINTER(PrefDesc), C.POINTER(sz)]
         L.tkv_dense_preference.argtypes = [C.POINTER(PrefDesc), vp, vp, i32, C.c_float, vp, vp, sz, vp]
         L.tkv_classify_layer.argtypes = [C.POINTER(C.c_float), i32, i32, C.c_float, C.POINTER(C.c_float)]
+        L.tkv_qk_norm_rope.argtypes = [C.POINTER(RopeDesc), i32] + [vp] * 11
         L.tkv_debug_quant_attn_config.argtypes = [i32, i32]
         L.tkv_debug_quant_attn_config.restype = i32
         L.tkv_debug_read_sweep.argtypes = [vp, C.c_size_t, vp, i32, vp]
@@ -119,7 +127,7 @@ def lib() -> C.CDLL:
                      "tkv_sparse_prefetch_keys", "tkv_sparse_estimate_topk_cm",
                      "tkv_sparse_select_estimate_topk", "tkv_sparse_append_dynamic",
                      "tkv_sparse_append_estimate_topk", "tkv_sparse_decode", "tkv_dense_preference_sizes", "tkv_dense_preference",
-                     "tkv_classify_layer"):
+                     "tkv_classify_layer", "tkv_qk_norm_rope"):
             getattr(L, name).restype = C.c_int32
         _LIB = L
     return _LIB
@@ -146,6 +154,12 @@ def _stream(stream) -> int:
     if stream is None:  # the current device's current stream; as an object it costs 2.8 us, a quarter of a short step's call
         return torch._C._cuda_getCurrentRawStream(torch._C._cuda_getDevice())
     return stream.cuda_stream if hasattr(stream, "cuda_stream") else int(stream)
+
+
+def _on_current(t: torch.Tensor, stream) -> None:
+    """Without a stream the current device's is used: the tensors have to be that device's."""
+    assert stream is not None or t.device.index == torch._C._cuda_getDevice(), \
+        f"tensors on {t.device}, the current device is another: make it current or pass a stream of theirs"
 
 
 def _ptr(t) -> int:
@@ -511,6 +525,56 @@ class Stage1:
                                                  L.workspace.data_ptr(), L.workspace_bytes, _stream(stream)),
                "tkv_sparse_estimate_topk_cm")
         return L.topk_idx, L.topk_count
+
+
+_DTYPES = {torch.float16: 0, torch.bfloat16: 1}
+
+
+def qk_norm_rope(q: torch.Tensor, k: torch.Tensor, positions: torch.Tensor | None, inv_freq: torch.Tensor | None, *,
+                 v: torch.Tensor | None = None, norm: bool = False, q_weight: torch.Tensor | None = None,
+                 k_weight: torch.Tensor | None = None, eps: float = 1e-6, interleaved: bool = False,
+                 out_dtype: torch.dtype | None = None, q_out: torch.Tensor | None = None,
+                 k_out: torch.Tensor | None = None, v_out: torch.Tensor | None = None, stream=None):
+    """tkv_qk_norm_rope: q [T, Hq, 128], k, v [T, Hkv, 128] (fp16 or bf16, views of one fused projection
+    allowed), positions int32 [T], inv_freq float32 [R/2] (None: no rotation) -> contiguous (q_out, k_out, v_out or
+    None) in out_dtype (default: the inputs')."""
+    assert q.is_cuda and q.dim() == 3 and k.dim() == 3 and k.shape[0] == q.shape[0] and k.shape[2] == q.shape[2]
+    _on_current(q, stream)
+    t, dt = q.shape[0], q.dtype
+    for x in (k, v, q_weight, k_weight):
+        assert x is None or (x.dtype == dt and x.device == q.device)
+    for x in (q, k, v):
+        assert x is None or x.stride(2) == 1
+    assert v is None or v.shape == k.shape
+    rot = 0
+    if inv_freq is not None:
+        assert inv_freq.dtype == torch.float32 and inv_freq.device == q.device and inv_freq.dim() == 1 and inv_freq.is_contiguous()
+        assert positions is not None and positions.dtype == torch.int32 and positions.device == q.device
+        assert tuple(positions.shape) == (t,) and positions.is_contiguous()
+        rot = 2 * inv_freq.shape[0]
+    for w in (q_weight, k_weight):
+        assert w is None or (tuple(w.shape) == (q.shape[2],) and w.is_contiguous())
+    if out_dtype is None:
+        out_dtype = next((x.dtype for x in (q_out, k_out, v_out) if x is not None), dt)
+    outs = []
+    for x, o in ((q, q_out), (k, k_out), (v, v_out)):
+        if x is None:
+            assert o is None
+        elif o is None:
+            o = torch.empty(x.shape, dtype=out_dtype, device=q.device)
+        else:
+            assert o.dtype == out_dtype and o.shape == x.shape and o.is_contiguous() and o.device == q.device
+        outs.append(o)
+
+    def strides(x):  # (an axis of one element: torch leaves its stride to chance)
+        return (C.c_int64 * 2)() if x is None else (C.c_int64 * 2)(x.stride(0) if t > 1 else 0, x.stride(1) if x.shape[1] > 1 else 0)
+
+    desc = RopeDesc(C.sizeof(RopeDesc), q.shape[1], k.shape[1], q.shape[2], _DTYPES.get(dt, -1), _DTYPES.get(out_dtype, -1),
+                    int(norm), float(eps), rot, int(interleaved), strides(q), strides(k), strides(v))
+    _check(lib().tkv_qk_norm_rope(C.byref(desc), t, q.data_ptr(), k.data_ptr(), _ptr(v), _ptr(positions) if rot else 0,
+                                  _ptr(inv_freq) if rot else 0, _ptr(q_weight), _ptr(k_weight), outs[0].data_ptr(), outs[1].data_ptr(),
+                                  _ptr(outs[2]), _stream(stream)), "tkv_qk_norm_rope")
+    return tuple(outs)
 
 
 class DensePreference:
