@@ -469,6 +469,45 @@ int32_t tkv_qk_norm_rope(const tkv_rope_desc* desc, int32_t n_tokens, const void
                          const int32_t* positions, const float* inv_freq, const void* q_weight, const void* k_weight,
                          void* q_out, void* k_out, void* v_out, void* stream);
 
+typedef struct {
+  uint32_t struct_size; /* sizeof(tkv_prompt_desc)                                        */
+  int32_t n_q_heads;    /* Hq, at most 1024; a multiple of n_kv_heads, any multiple       */
+  int32_t n_kv_heads;
+  int32_t head_dim;     /* 128                                                            */
+  int32_t dtype;        /* tkv_dtype of q, k, v and out                                   */
+  int32_t causal;       /* 1: a token sees the keys up to its own; 0: all of its sequence */
+  int32_t batch;        /* sequences, 1..TKV_MAX_BATCH                                    */
+  int32_t reserved;     /* 0                                                              */
+  int64_t q_stride[2];  /* strides of tokens and heads in elements, multiples of 8, that of */
+  int64_t k_stride[2];  /* tokens at most 2^22; the 128 channels of a row lie side by side  */
+  int64_t v_stride[2];
+  int64_t o_stride[2];
+} tkv_prompt_desc;
+
+/* Workspace bytes of tkv_prompt_attn: 65 MiB whatever the descriptor (partial results of 1024 tiles of 128 rows). */
+int32_t tkv_prompt_attn_sizes(const tkv_prompt_desc* desc, size_t* workspace_bytes);
+
+/*
+ * Eq. 3 over unquantized rows for many tokens at once: the attention that a prompt's own pass needs before its
+ * keys and values go into a cache.  Sequence b has q_len[b] query tokens, rows q_start[b] on of q and out, and k_len[b] keys and
+ * values, rows k_start[b] on of k and v (HOST int32 [B] arrays each): packed sequences, padded batches and
+ * chunks alike.  The queries are the sequence's last tokens: token i of them sees the keys j <= i + k_len - q_len
+ * (causal) or all k_len.  So q_len = k_len is a whole prompt, q_len < k_len a chunk of it over what came before, or single
+ * tokens.  out = softmax(sm_scale q.k) v over the keys seen; a token that sees none yields zeros, and -inf in lse.
+ * q [.][Hq][128], k, v [.][Hkv][128], out [.][Hq][128] with the descriptor's strides; query head i reads KV head i / (Hq/Hkv).
+ * lse: float32 [rows of q][Hq] contiguous, the natural logarithm of the sum of exponentials, or NULL.  Rows of out
+ * and lse that belong to no sequence are left as they were, rows of k and v behind a sequence's last are not used (whatever they
+ * hold).  A non-finite value in a row that a query does not see may still reach it where both lie in the same 64 keys.
+ * out must not overlap the inputs; sequences must not share rows of out.  sm_scale > 0 (TKV_E_INVAL otherwise).
+ * Products in the inputs' type with float32 sums; softmax statistics and sums in float32, its weights rounded to the
+ * inputs' type for the second product.  The result is the same bit for bit from call to call.
+ * Few rows over many keys are split over the keys and joined from partial results in `workspace` (any
+ * contents; 16-byte aligned; concurrent calls need separate ones).
+ */
+int32_t tkv_prompt_attn(const tkv_prompt_desc* desc, const void* q, const void* k, const void* v, void* out, float* lse,
+                        const int32_t* q_start_host, const int32_t* q_len_host, const int32_t* k_start_host,
+                        const int32_t* k_len_host, float sm_scale, void* workspace, size_t workspace_bytes, void* stream);
+
 /* ---------------------------------------------------------------------------------
  * Offline identification (Sec. 4.1): which layers are quantization-friendly
  * ------------------------------------------------------------------------------- */

@@ -65,6 +65,13 @@ class RopeDesc(C.Structure):
                 ("q_stride", C.c_int64 * 2), ("k_stride", C.c_int64 * 2), ("v_stride", C.c_int64 * 2)]
 
 
+class PromptDesc(C.Structure):
+    _fields_ = [("struct_size", C.c_uint32), ("n_q_heads", C.c_int32), ("n_kv_heads", C.c_int32),
+                ("head_dim", C.c_int32), ("dtype", C.c_int32), ("causal", C.c_int32), ("batch", C.c_int32),
+                ("reserved", C.c_int32), ("q_stride", C.c_int64 * 2), ("k_stride", C.c_int64 * 2),
+                ("v_stride", C.c_int64 * 2), ("o_stride", C.c_int64 * 2)]
+
+
 def lib() -> C.CDLL:
     """Loads libtkv.so (built by paper_2505_19586_amd/build.py); raises if absent."""
     global _LIB
@@ -114,6 +121,8 @@ def lib() -> C.CDLL:
         L.tkv_dense_preference.argtypes = [C.POINTER(PrefDesc), vp, vp, i32, C.c_float, vp, vp, sz, vp]
         L.tkv_classify_layer.argtypes = [C.POINTER(C.c_float), i32, i32, C.c_float, C.POINTER(C.c_float)]
         L.tkv_qk_norm_rope.argtypes = [C.POINTER(RopeDesc), i32] + [vp] * 11
+        L.tkv_prompt_attn_sizes.argtypes = [C.POINTER(PromptDesc), C.POINTER(sz)]
+        L.tkv_prompt_attn.argtypes = [C.POINTER(PromptDesc)] + [vp] * 5 + [C.POINTER(i32)] * 4 + [C.c_float, vp, sz, vp]
         L.tkv_debug_quant_attn_config.argtypes = [i32, i32]
         L.tkv_debug_quant_attn_config.restype = i32
         L.tkv_debug_read_sweep.argtypes = [vp, C.c_size_t, vp, i32, vp]
@@ -127,7 +136,8 @@ def lib() -> C.CDLL:
                      "tkv_sparse_prefetch_keys", "tkv_sparse_estimate_topk_cm",
                      "tkv_sparse_select_estimate_topk", "tkv_sparse_append_dynamic",
                      "tkv_sparse_append_estimate_topk", "tkv_sparse_decode", "tkv_dense_preference_sizes", "tkv_dense_preference",
-                     "tkv_classify_layer", "tkv_qk_norm_rope"):
+                     "tkv_classify_layer", "tkv_qk_norm_rope",
+                     "tkv_prompt_attn_sizes", "tkv_prompt_attn"):
             getattr(L, name).restype = C.c_int32
         _LIB = L
     return _LIB
@@ -575,6 +585,66 @@ def qk_norm_rope(q: torch.Tensor, k: torch.Tensor, positions: torch.Tensor | Non
                                   _ptr(inv_freq) if rot else 0, _ptr(q_weight), _ptr(k_weight), outs[0].data_ptr(), outs[1].data_ptr(),
                                   _ptr(outs[2]), _stream(stream)), "tkv_qk_norm_rope")
     return tuple(outs)
+
+
+class PromptAttention:
+    """Attention over whole prompts, packed sequences and chunks (tkv_prompt_attn): the workspace and the call."""
+
+    def __init__(self, *, n_q_heads=32, n_kv_heads=8, head_dim=128, dtype=torch.float16, causal=True, batch=1,
+                 device="cuda:0"):
+        dev = _require_gpu(device)
+        self.desc = PromptDesc(C.sizeof(PromptDesc), n_q_heads, n_kv_heads, head_dim, _DTYPES.get(dtype, -1), int(causal), batch, 0)
+        ws = C.c_size_t()
+        _check(lib().tkv_prompt_attn_sizes(C.byref(self.desc), C.byref(ws)), "tkv_prompt_attn_sizes")
+        self.workspace_bytes = int(ws.value)
+        self.workspace = torch.empty(self.workspace_bytes, dtype=torch.uint8, device=dev)
+        self.dtype = dtype
+        self.device = dev
+
+    def attend(self, q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, sm_scale: float, q_lens, k_lens=None, *,
+               q_starts=None, k_starts=None, out: torch.Tensor | None = None, lse: bool | torch.Tensor = False, stream=None):
+        """q [Tq, Hq, 128], k, v [Tk, Hkv, 128] (views of wider rows allowed); q_lens, k_lens (default: q_lens): tokens of
+        every sequence, one after the other unless q_starts / k_starts say where each begins.  Returns out
+        [Tq, Hq, 128], or (out, lse [Tq, Hq]) where lse is True or a float32 tensor.  Rows of no sequence are left as they
+        were (a new out has zeros there)."""
+        d = self.desc
+        assert q.is_cuda and q.dim() == 3 and k.dim() == 3 and k.shape == v.shape
+        assert q.dtype == k.dtype == v.dtype == self.dtype and q.device == k.device == v.device == self.workspace.device
+        assert tuple(q.shape[1:]) == (d.n_q_heads, d.head_dim) and tuple(k.shape[1:]) == (d.n_kv_heads, d.head_dim)
+        assert q.stride(2) == 1 and k.stride(2) == 1 and v.stride(2) == 1
+        _on_current(q, stream)
+        lens = np.empty((4, d.batch), dtype=np.int32)   # q_start, q_len, k_start, k_len
+        lens[1] = q_lens
+        lens[3] = q_lens if k_lens is None else k_lens
+        rows = (q.shape[0], 0, k.shape[0])
+        packed = q_starts is None
+        for i, given in ((0, q_starts), (2, k_starts)):
+            if given is None:
+                lens[i, 0] = 0
+                np.cumsum(lens[i + 1, :-1], out=lens[i, 1:])
+            else:
+                lens[i] = given
+            assert lens[i].min() >= 0 and lens[i + 1].min() >= 0
+            assert int((lens[i].astype(np.int64) + lens[i + 1]).max()) <= rows[i], "a sequence reaches past the tensor's rows"
+        if out is None:
+            out = (torch.empty if packed and int(lens[1].sum()) == q.shape[0] else torch.zeros)(q.shape, dtype=q.dtype, device=q.device)
+        else:
+            assert out.dtype == q.dtype and out.shape == q.shape and out.device == q.device and out.stride(2) == 1
+        if lse is True:
+            lse = torch.full(q.shape[:2], -float("inf"), dtype=torch.float32, device=q.device) if not packed or int(lens[1].sum()) != q.shape[0] \
+                else torch.empty(q.shape[:2], dtype=torch.float32, device=q.device)
+        elif lse is False or lse is None:
+            lse = None
+        else:
+            assert lse.dtype == torch.float32 and lse.shape == q.shape[:2] and lse.is_contiguous() and lse.device == q.device
+        for s, x in ((d.q_stride, q), (d.k_stride, k), (d.v_stride, v), (d.o_stride, out)):
+            s[0] = x.stride(0) if x.shape[0] > 1 else 0   # (an axis of one element: torch leaves its stride to chance)
+            s[1] = x.stride(1) if x.shape[1] > 1 else 0
+        at = [lens[i].ctypes.data_as(C.POINTER(C.c_int32)) for i in range(4)]
+        _check(lib().tkv_prompt_attn(C.byref(d), q.data_ptr(), k.data_ptr(), v.data_ptr(), out.data_ptr(), _ptr(lse), *at,
+                                     float(sm_scale), self.workspace.data_ptr(), self.workspace_bytes, _stream(stream)),
+               "tkv_prompt_attn")
+        return out if lse is None else (out, lse)
 
 
 class DensePreference:
