@@ -216,6 +216,27 @@ int32_t tkv_quant_decode(const tkv_quant_desc* desc, tkv_quant_cache* cache, con
 int32_t tkv_quant_attn_decode_static(const tkv_quant_desc* desc, const tkv_quant_cache* cache, const void* q,
                                      void* out, float sm_scale, void* stream);
 
+/* Workspace bytes of tkv_quant_attn_decode_shared for these prefix and batch descriptors (any contents before a call). */
+int32_t tkv_quant_attn_decode_shared_sizes(const tkv_quant_desc* prefix_desc, const tkv_quant_desc* desc, size_t* workspace_bytes);
+
+/*
+ * Eq. 3 for a batch whose sequences share long prefixes (a system prompt, a document): sequence b's tokens are those of
+ * sequence prefix_of_host[b] of `prefix` (HOST int32 [B]; -1: none; NULL: 0 for all) followed by its own in `cache`, one softmax over
+ * all of them.  The prefixes are ordinary quantized caches, filled by tkv_quantize_append and held once; each is read once for
+ * all of its sequences (64 rows, a row being a query head of a KV head, at a time).  The result is that of
+ * tkv_quant_attn_decode over a cache that held prefix and own tokens, quantized as they are here: the prefix's
+ * newest tokens stay fp16 as its own descriptor says.
+ * prefix_desc and desc: same heads, bits and group_size; residual, capacity and batch may differ.  Either may hold empty
+ * sequences; a sequence without any token yields zeros.  q (a multiple of 4 bytes), out: fp16 [B][Hq][128].  sm_scale > 0.
+ * All six settings of bits and group_size are evaluated alike: code*s + z rounded to fp16, products of fp16 numbers with float32
+ * sums, softmax statistics in float32, its weights rounded to fp16.  Cached values of magnitude up to 30000 are safe (a
+ * dequantized value beyond 65504 is infinite).  The result is the same bit for bit from call to call.
+ * Partial results go through `workspace` (16-byte aligned; concurrent calls need separate ones).
+ */
+int32_t tkv_quant_attn_decode_shared(const tkv_quant_desc* prefix_desc, const tkv_quant_cache* prefix, const tkv_quant_desc* desc,
+                                     const tkv_quant_cache* cache, const int32_t* prefix_of_host, const void* q, void* out,
+                                     float sm_scale, void* workspace, size_t workspace_bytes, void* stream);
+
 /* ---------------------------------------------------------------------------------
  * Sparsity-friendly layers
  * ------------------------------------------------------------------------------- */

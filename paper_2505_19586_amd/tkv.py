@@ -123,6 +123,9 @@ def lib() -> C.CDLL:
         L.tkv_qk_norm_rope.argtypes = [C.POINTER(RopeDesc), i32] + [vp] * 11
         L.tkv_prompt_attn_sizes.argtypes = [C.POINTER(PromptDesc), C.POINTER(sz)]
         L.tkv_prompt_attn.argtypes = [C.POINTER(PromptDesc)] + [vp] * 5 + [C.POINTER(i32)] * 4 + [C.c_float, vp, sz, vp]
+        L.tkv_quant_attn_decode_shared_sizes.argtypes = [C.POINTER(QuantDesc), C.POINTER(QuantDesc), C.POINTER(sz)]
+        L.tkv_quant_attn_decode_shared.argtypes = [C.POINTER(QuantDesc), C.POINTER(QuantCache), C.POINTER(QuantDesc),
+                                                   C.POINTER(QuantCache), C.POINTER(i32), vp, vp, C.c_float, vp, sz, vp]
         L.tkv_debug_quant_attn_config.argtypes = [i32, i32]
         L.tkv_debug_quant_attn_config.restype = i32
         L.tkv_debug_read_sweep.argtypes = [vp, C.c_size_t, vp, i32, vp]
@@ -137,7 +140,8 @@ def lib() -> C.CDLL:
                      "tkv_sparse_select_estimate_topk", "tkv_sparse_append_dynamic",
                      "tkv_sparse_append_estimate_topk", "tkv_sparse_decode", "tkv_dense_preference_sizes", "tkv_dense_preference",
                      "tkv_classify_layer", "tkv_qk_norm_rope",
-                     "tkv_prompt_attn_sizes", "tkv_prompt_attn"):
+                     "tkv_prompt_attn_sizes", "tkv_prompt_attn", "tkv_quant_attn_decode_shared_sizes",
+                     "tkv_quant_attn_decode_shared"):
             getattr(L, name).restype = C.c_int32
         _LIB = L
     return _LIB
@@ -282,6 +286,42 @@ class QuantLayer:
         if name in ("v_scale", "v_zero"):
             return buf.view(torch.float16).view(*bh, j, 128 // d.group_size, 32)
         return buf.view(torch.float16).view(*bh, d.residual + d.group_size, 128)
+
+
+class SharedPrefix:
+    """Decode attention of a batch (`layer`) whose sequences share prefixes, each held once in `prefix`
+    (tkv_quant_attn_decode_shared).  Both are ordinary QuantLayers: append a prompt to `prefix`, every sequence's own
+    tokens to `layer`."""
+
+    def __init__(self, prefix: QuantLayer, layer: QuantLayer):
+        ws = C.c_size_t()
+        _check(lib().tkv_quant_attn_decode_shared_sizes(C.byref(prefix.desc), C.byref(layer.desc), C.byref(ws)),
+               "tkv_quant_attn_decode_shared_sizes")
+        assert prefix.workspace.device == layer.workspace.device
+        self.prefix, self.layer = prefix, layer
+        self.workspace_bytes = int(ws.value)
+        self.workspace = torch.empty(self.workspace_bytes, dtype=torch.uint8, device=layer.device)
+
+    def attn_decode(self, q: torch.Tensor, sm_scale: float, prefix_of=None, out: torch.Tensor | None = None, stream=None):
+        """q fp16 [B, Hq, 128]; prefix_of: for every sequence the prefix it continues, -1 for none (default: 0 for all)."""
+        d = self.layer.desc
+        assert q.dtype == torch.float16 and q.is_contiguous() and tuple(q.shape) == (d.batch, d.n_q_heads, d.head_dim)
+        assert q.device == self.workspace.device
+        _on_current(q, stream)
+        of = None
+        if prefix_of is not None:
+            of = np.ascontiguousarray(prefix_of, dtype=np.int32)
+            assert of.shape == (d.batch,)
+        if out is None:
+            out = torch.empty_like(q)
+        else:
+            assert out.dtype == torch.float16 and out.is_contiguous() and out.shape == q.shape and out.device == q.device
+        _check(lib().tkv_quant_attn_decode_shared(C.byref(self.prefix.desc), C.byref(self.prefix.cache), C.byref(d),
+                                                  C.byref(self.layer.cache),
+                                                  None if of is None else of.ctypes.data_as(C.POINTER(C.c_int32)), q.data_ptr(),
+                                                  out.data_ptr(), float(sm_scale), self.workspace.data_ptr(), self.workspace_bytes,
+                                                  _stream(stream)), "tkv_quant_attn_decode_shared")
+        return out
 
 
 class SparseLayer:
