@@ -505,7 +505,7 @@ typedef struct {
   int64_t o_stride[2];
 } tkv_prompt_desc;
 
-/* Workspace bytes of tkv_prompt_attn: 65 MiB whatever the descriptor (partial results of 1024 tiles of 128 rows). */
+/* Workspace bytes of tkv_prompt_attn: 32.5 MiB whatever the descriptor (partial results of 256 tiles of 256 rows). */
 int32_t tkv_prompt_attn_sizes(const tkv_prompt_desc* desc, size_t* workspace_bytes);
 
 /*

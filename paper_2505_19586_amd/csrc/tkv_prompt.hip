@@ -24,13 +24,17 @@ typedef _Float16 half8 __attribute__((ext_vector_type(8)));
 typedef __bf16 bhalf8 __attribute__((ext_vector_type(8)));
 
 constexpr int kKeys = 64;       // keys of a tile
-constexpr int kRows = 128;      // rows of a workgroup: four waves of 32
-constexpr int kMaxParts = 1024; // partial results that the workspace has room for
+constexpr int kWaves = 8;
+constexpr int kRows = 32 * kWaves;  // rows of a workgroup
+constexpr int kMaxParts = 256;      // partial results that the workspace has room for
+constexpr int kWorkgroups = 256;     // compute units
+static_assert(kWorkgroups <= kMaxParts, "a split launch's workgroups write a part each");
 constexpr int kPartFloats = kRows * (TKV_D + 2);
-// Weights are 2^(logit - reference + kShift): the reference follows the running maximum only when that
-// is kLazy above it, so the largest weight is 2^(kLazy + kShift) = 2^15, inside fp16's range, and fp16's subnormal numbers begin 2^-21 below
-// the reference's weight, not 2^-14.
-constexpr float kLazy = 8.f, kShift = 7.f;
+// Weights are 2^(logit - reference + kShift): the reference follows the running maximum only when a weight is above 2^15, inside
+// fp16's range, and fp16's subnormal numbers begin 2^-21 below the reference's weight, not 2^-14.
+constexpr float kShift = 7.f;
+template <typename T>
+constexpr uint32_t too_large() { return __is_same(T, _Float16) ? 0x7800u : 0x4700u; }  // 2^15's bits
 constexpr float kNone = -1e30f;  // reference of a row without a key so far
 
 struct PromptSeq {
@@ -43,7 +47,8 @@ struct PromptParams {
   const void* v;
   void* out;
   float* lse;    // NULL: not wanted
-  float* parts;  // [part][kRows][128] weighted sums, then [part][kRows][2] (reference, sum)
+  float* parts;  // [part][rows of a tile][128] weighted sums
+  float* ml;     // [part][rows of a tile][2] (reference, sum)
   int64_t q_st, q_sh, k_st, k_sh, v_st, v_sh, o_st, o_sh;
   int32_t hq, hkv, group, batch, causal;
   float scale2;  // sm_scale * log2(e)
@@ -51,6 +56,8 @@ struct PromptParams {
   int32_t first_item[TKV_MAX_BATCH];  // in (row tile, piece) pairs
   int32_t first_part[TKV_MAX_BATCH];  // -1: the sequence's rows are not split
   int32_t pieces[TKV_MAX_BATCH];
+  int32_t first_row[TKV_MAX_BATCH];   // of the split sequences' rows (of one KV head), for the joining launch
+  int32_t tile_rows;                  // rows of a tile: kRows, or kFew
 };
 
 template <typename T>
@@ -69,13 +76,13 @@ __device__ inline uintx4 pack8(floatx8 x) {
 
 typedef __attribute__((address_space(3))) char lds_char;
 
-__device__ inline uintx4 lds_read16(uint32_t at) {
-  return *(__attribute__((address_space(3))) uintx4*)(lds_char*)(uintptr_t)at;
+__device__ inline uintx4 lds_read16(lds_char* at) {
+  return *(__attribute__((address_space(3))) uintx4*)at;
 }
 // 4 x 16 elements transposed over sixteen lanes: lane 4 r + c of the sixteen names row r's columns 4 c to 4 c + 3,
 // lane c receives column c of the four rows.
-__device__ inline uintx2 lds_read_tr(uint32_t at) {
-  return __builtin_bit_cast(uintx2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) shortx4*)(lds_char*)(uintptr_t)at));
+__device__ inline uintx2 lds_read_tr(lds_char* at) {
+  return __builtin_bit_cast(uintx2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) shortx4*)at));
 }
 
 // 16 bytes per lane from a descriptor's array straight to LDS, in lane order from `to` (uniform) on.  By hand, because the
@@ -109,12 +116,17 @@ __device__ inline Item find_item(const PromptParams& p, int it) {
   return x;
 }
 
+// A wave's work on a tile of 64 keys is two products on the matrix cores and the softmax between them on the vector units, about
+// 1024 and 900 cycles.  Two waves of a SIMD left to themselves fall into step and wait for the same unit, so the workgroup's two halves
+// (waves 0 to 3 and 4 to 7: one of each on every SIMD) take turns: while one multiplies (the weights of its last tile with the
+// values, the queries with the next keys), the other works out weights, and a barrier changes the parts.
 template <typename T>
-__global__ __launch_bounds__(256, 2) void prompt_attn_kernel(PromptParams p) {
-  __shared__ __attribute__((aligned(1024))) char lds[2 * 2 * kKeys * TKV_D * 2];  // two buffers of a K and a V tile
+__global__ __launch_bounds__(64 * kWaves, 2) void prompt_attn_kernel(PromptParams p) {
+  __shared__ __attribute__((aligned(1024))) char lds[2 * 2 * kKeys * TKV_D * 2];  // two K tiles, two V tiles
   constexpr int kTile = kKeys * TKV_D * 2;
   const int lane = threadIdx.x % 64, half = lane / 32, col = lane % 32;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
+  const int late = wave / (kWaves / 2);
   const int h = blockIdx.x % p.hkv;
   const Item it = find_item(p, blockIdx.x / p.hkv);
   const PromptSeq sq = p.seq[it.b];
@@ -135,6 +147,7 @@ __global__ __launch_bounds__(256, 2) void prompt_attn_kernel(PromptParams p) {
   const int limit_low = p.causal ? w_first / p.group + ahead : sq.k_len - 1;
   const int limit_high = p.causal ? w_last / p.group + ahead : sq.k_len - 1;
   const bool wave_on = it.tile * kRows + 32 * wave < rows;
+  const int my_end = wave_on ? min(t1, limit_high / kKeys + (limit_high >= 0 ? 1 : 0)) : t0;  // the wave has work in [t0, my_end)
 
   uintx4 qf[8];
   {
@@ -145,31 +158,32 @@ __global__ __launch_bounds__(256, 2) void prompt_attn_kernel(PromptParams p) {
 
   // staging: an instruction of a wave brings four rows; LDS keeps a row's sixteen 16-byte places in an order that depends on the
   // row, so that the reads below (a column of keys, a block of four keys) meet all banks
-  uint32_t k_off[4], v_off[4];
+  constexpr int kLoads = 16 / kWaves;  // per wave and tile of keys or values
+  uint32_t k_off[kLoads], v_off[kLoads];
 #pragma unroll
-  for (int j = 0; j < 4; ++j) {
-    const int r = 16 * wave + 4 * j + lane / 16, place = lane % 16;
+  for (int j = 0; j < kLoads; ++j) {
+    const int r = 4 * (kLoads * wave + j) + lane / 16, place = lane % 16;
     k_off[j] = (uint32_t)(r * p.k_st * 2) + 16u * (uint32_t)(place ^ (r & 15));
     v_off[j] = (uint32_t)(r * p.v_st * 2) + 16u * (uint32_t)(place ^ (((r & 3) << 2) | ((r >> 2) & 3)));
   }
   const char* k_base = (const char*)p.k + ((int64_t)sq.k_start * p.k_st + (int64_t)h * p.k_sh) * 2;
   const char* v_base = (const char*)p.v + ((int64_t)sq.k_start * p.v_st + (int64_t)h * p.v_sh) * 2;
   const uint32_t lds0 = (uint32_t)(uintptr_t)(lds_char*)lds;
-  auto stage = [&](int t, int buf) {
+  auto stage = [&](const char* base, int64_t st, const uint32_t (&off)[kLoads], int t, uint32_t to) {
     const int left = min(kKeys, sq.k_len - t * kKeys);  // rows behind the sequence's last read as zeros
-    const auto kr = __builtin_amdgcn_make_buffer_rsrc((void*)(k_base + (int64_t)t * kKeys * p.k_st * 2), 0, (int)((left - 1) * p.k_st * 2 + TKV_D * 2), 0x00020000);
-    const auto vr = __builtin_amdgcn_make_buffer_rsrc((void*)(v_base + (int64_t)t * kKeys * p.v_st * 2), 0, (int)((left - 1) * p.v_st * 2 + TKV_D * 2), 0x00020000);
-    const uint32_t to = lds0 + (uint32_t)(buf * 2 * kTile + wave * 4096);
+    const auto r = __builtin_amdgcn_make_buffer_rsrc((void*)(base + (int64_t)t * kKeys * st * 2), 0, (int)((left - 1) * st * 2 + TKV_D * 2), 0x00020000);
 #pragma unroll
-    for (int j = 0; j < 4; ++j) to_lds(kr, to + 1024 * j, k_off[j]);
-#pragma unroll
-    for (int j = 0; j < 4; ++j) to_lds(vr, to + kTile + 1024 * j, v_off[j]);
+    for (int j = 0; j < kLoads; ++j) to_lds(r, to + 1024 * (kLoads * wave + j), off[j]);
   };
+  // K tile t goes to buffer t - t0 mod 2, V tile t to the two behind; everyone has left a buffer two turns before it is filled again
+  auto stage_k = [&](int t) { if (t < t1) stage(k_base, p.k_st, k_off, t, lds0 + ((t - t0) & 1) * kTile); };
+  auto stage_v = [&](int t) { if (t < t1) stage(v_base, p.v_st, v_off, t, lds0 + (2 + ((t - t0) & 1)) * kTile); };
 
-  // LDS addresses of the operands, without buffer, key step and tile
-  uint32_t ka[8], va[8];
+  // LDS places of the operands, without buffer, key step and tile
+  lds_char* ka[8];
+  lds_char* va[8];
 #pragma unroll
-  for (int kk = 0; kk < 8; ++kk) ka[kk] = lds0 + (uint32_t)(col * 256 + 16 * ((2 * kk + half) ^ (col & 15)));
+  for (int kk = 0; kk < 8; ++kk) ka[kk] = (lds_char*)lds + (col * 256 + 16 * ((2 * kk + half) ^ (col & 15)));
   {
     const int l16 = lane % 16, right = (lane / 16) % 2;
 #pragma unroll
@@ -178,30 +192,20 @@ __global__ __launch_bounds__(256, 2) void prompt_attn_kernel(PromptParams p) {
       for (int s = 0; s < 2; ++s) {
         const int key = 8 * s + 4 * half + l16 / 4;
         const int place = (4 * dt + 2 * right + (l16 % 4) / 2) ^ (((key & 3) << 2) | ((key >> 2) & 3));
-        va[2 * dt + s] = lds0 + (uint32_t)(kTile + key * 256 + 16 * place + 8 * (l16 % 2));
+        va[2 * dt + s] = (lds_char*)lds + (2 * kTile + key * 256 + 16 * place + 8 * (l16 % 2));
       }
   }
 
-  floatx16 o[4];
+  floatx16 o[4], s[2];
+  uintx4 pf[4];
 #pragma unroll
   for (int dt = 0; dt < 4; ++dt)
 #pragma unroll
     for (int i = 0; i < 16; ++i) o[dt][i] = 0.f;
   float ref = kNone, sum = 0.f;
 
-  // (The query rows are waited for here: the compiler, which does not know of the loads to LDS, would wait for them and those
-  // inside the loop.)
-#pragma unroll
-  for (int kk = 0; kk < 8; ++kk) asm volatile("" : "+v"(qf[kk]));
-  if (t0 < t1) stage(t0, 0);
-  for (int t = t0; t < t1; ++t) {
-    const int buf = (t - t0) & 1;
-    asm volatile("s_waitcnt vmcnt(0)\n\ts_barrier" ::: "memory");  // the tile is there, everyone is done with the other buffer
-    if (t + 1 < t1) stage(t + 1, buf ^ 1);
-    const int key0 = t * kKeys;
-    if (!wave_on || key0 > limit_high) continue;
-    const uint32_t at = (uint32_t)(buf * 2 * kTile);
-    floatx16 s[2];
+  auto logits = [&](int t) {  // of tile t, into s
+    const int at = ((t - t0) & 1) * kTile;
 #pragma unroll
     for (int y = 0; y < 2; ++y)
 #pragma unroll
@@ -210,36 +214,9 @@ __global__ __launch_bounds__(256, 2) void prompt_attn_kernel(PromptParams p) {
     for (int kk = 0; kk < 8; ++kk)
 #pragma unroll
       for (int y = 0; y < 2; ++y) s[y] = mfma32<T>(lds_read16(ka[kk] + at + 8192 * y), qf[kk], s[y]);
-    if (key0 + kKeys - 1 > limit_low || key0 + kKeys > sq.k_len) {
-#pragma unroll
-      for (int y = 0; y < 2; ++y)
-#pragma unroll
-        for (int i = 0; i < 16; ++i)
-          s[y][i] = key0 + 32 * y + 8 * (i / 4) + 4 * half + i % 4 <= limit ? s[y][i] : -INFINITY;
-    }
-    float top = fmaxf(s[0][0], s[1][0]);
-#pragma unroll
-    for (int i = 1; i < 16; ++i) top = fmaxf(top, fmaxf(s[0][i], s[1][i]));
-    top = fmaxf(top, other_half(top, half)) * p.scale2;
-    if (__builtin_amdgcn_ballot_w64(top > ref + kLazy) != 0) {
-      const float next = fmaxf(ref, top), shrink = __builtin_amdgcn_exp2f(ref - next);
-      ref = next;
-      sum *= shrink;
-#pragma unroll
-      for (int dt = 0; dt < 4; ++dt) o[dt] *= shrink;
-    }
-    const float less = kShift - ref;
-    uintx4 pf[4];
-#pragma unroll
-    for (int y = 0; y < 2; ++y) {
-#pragma unroll
-      for (int i = 0; i < 16; ++i) {
-        s[y][i] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[y][i], p.scale2, less));
-        sum += s[y][i];
-      }
-      pf[2 * y] = pack8<T>(__builtin_shufflevector(s[y], s[y], 0, 1, 2, 3, 4, 5, 6, 7));
-      pf[2 * y + 1] = pack8<T>(__builtin_shufflevector(s[y], s[y], 8, 9, 10, 11, 12, 13, 14, 15));
-    }
+  };
+  auto products = [&](int t) {  // the weights of tile t with its values
+    const int at = ((t - t0) & 1) * kTile;
 #pragma unroll
     for (int ks = 0; ks < 4; ++ks)
 #pragma unroll
@@ -248,16 +225,103 @@ __global__ __launch_bounds__(256, 2) void prompt_attn_kernel(PromptParams p) {
         const uintx4 vf = __builtin_shufflevector(lo, hi, 0, 1, 2, 3);
         o[dt] = mfma32<T>(vf, pf[ks], o[dt]);
       }
+  };
+  auto weights = [&](int t) {
+    const int key0 = t * kKeys;
+    if (key0 + kKeys - 1 > limit_low || key0 + kKeys > sq.k_len) {
+#pragma unroll
+      for (int y = 0; y < 2; ++y)
+#pragma unroll
+        for (int i = 0; i < 16; ++i)
+          s[y][i] = key0 + 32 * y + 8 * (i / 4) + 4 * half + i % 4 <= limit ? s[y][i] : -INFINITY;
+    }
+    // The weights at once: they are positive, so their bits compare as numbers, two at a time, and the logits' maximum is worked out
+    // only where one is too large.
+    typedef uint16_t ushort2_t __attribute__((ext_vector_type(2)));
+    float part;
+    auto weigh = [&] {
+      const float less = kShift - ref;
+      part = 0.f;
+#pragma unroll
+      for (int y = 0; y < 4; ++y) {
+        floatx8 e;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          e[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[y / 2][8 * (y % 2) + i], p.scale2, less));
+          part += e[i];
+        }
+        pf[y] = pack8<T>(e);
+      }
+    };
+    weigh();
+    ushort2_t large = {0, 0};
+#pragma unroll
+    for (int y = 0; y < 4; ++y)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const uint32_t x = pf[y][i];
+        large = __builtin_elementwise_max(large, __builtin_bit_cast(ushort2_t, x));
+      }
+    if (__builtin_amdgcn_ballot_w64(max((uint32_t)large.x, (uint32_t)large.y) > too_large<T>()) != 0) {
+      float top = fmaxf(s[0][0], s[1][0]);
+#pragma unroll
+      for (int i = 1; i < 16; ++i) top = fmaxf(top, fmaxf(s[0][i], s[1][i]));
+      top = fmaxf(top, other_half(top, half)) * p.scale2;
+      const float next = fmaxf(ref, top), shrink = __builtin_amdgcn_exp2f(ref - next);
+      ref = next;
+      sum *= shrink;
+#pragma unroll
+      for (int dt = 0; dt < 4; ++dt) o[dt] *= shrink;
+      weigh();
+    }
+    sum += part;
+  };
+
+  // (The query rows are waited for here: the compiler, which does not know of the loads to LDS, would wait for them and those
+  // inside the loop.)
+#pragma unroll
+  for (int kk = 0; kk < 8; ++kk) asm volatile("" : "+v"(qf[kk]));
+  stage_k(t0);
+  asm volatile("s_waitcnt vmcnt(0)\n\ts_barrier" ::: "memory");
+  // Turn 2 i: the early half multiplies (tile i), the late half works out weights (of i - 1); turn 2 i + 1: the other way round.  K tile
+  // i + 1 and V tile i are sent for at the beginning of turn 2 i and waited for at the end of turn 2 i + 1.
+  if (late) {
+    stage_k(t0 + 1);
+    stage_v(t0);
+    asm volatile("s_barrier" ::: "memory");
   }
+  for (int t = t0; t < t1; ++t) {
+    if (!late) {
+      stage_k(t + 1);
+      stage_v(t);
+    }
+    __builtin_amdgcn_s_setprio(1);
+    if (t > t0 && t - 1 < my_end) products(t - 1);
+    if (t < my_end) logits(t);
+    __builtin_amdgcn_s_setprio(0);
+    if (late) asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    __builtin_amdgcn_sched_barrier(0);
+    asm volatile("s_barrier" ::: "memory");
+    __builtin_amdgcn_sched_barrier(0);
+    if (late) {
+      stage_k(t + 2);
+      stage_v(t + 1);
+    }
+    if (t < my_end) weights(t);
+    if (!late) asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    __builtin_amdgcn_sched_barrier(0);
+    asm volatile("s_barrier" ::: "memory");
+    __builtin_amdgcn_sched_barrier(0);
+  }
+  if (t1 > t0 && t1 - 1 < my_end) products(t1 - 1);
+  if (!late) asm volatile("s_barrier" ::: "memory");  // (as many as the late half)
 
   sum += other_half(sum, half);
   if (!wave_on || row >= rows) return;
   if (p.first_part[it.b] >= 0) {
     const size_t part = (size_t)p.first_part[it.b] + ((size_t)it.tile * pieces + it.piece) * p.hkv + h;
     const int r = 32 * wave + col;
-    float* ml = p.parts + (size_t)kMaxParts * kRows * TKV_D + (part * kRows + r) * 2;
-    if (half == 0) *(float2*)ml = make_float2(ref, sum);
-    if (sum == 0.f) return;  // (its weighted sum is not read)
+    if (half == 0) *(float2*)(p.ml + (part * kRows + r) * 2) = make_float2(ref, sum);
     float* to = p.parts + (part * kRows + r) * TKV_D;
 #pragma unroll
     for (int dt = 0; dt < 4; ++dt)
@@ -281,49 +345,252 @@ __global__ __launch_bounds__(256, 2) void prompt_attn_kernel(PromptParams p) {
         sum == 0.f ? -INFINITY : (ref - kShift + __builtin_amdgcn_logf(sum)) * 0.69314718055994531f;
 }
 
-// Joins the pieces of the split rows: a wave per row, blockIdx.y the row tile's quads of rows.
+// Few rows (single tokens, a few tokens of few heads: up to 32 of a sequence and KV head).  The keys' bytes bound this:
+// every wave takes 32-key tiles of its own through a ring of two of its own, with no barrier until the waves join.
+constexpr int kFew = 32, kFewWaves = 4, kFewKeys = 32;
+
+template <typename T>
+__global__ __launch_bounds__(64 * kFewWaves, 1) void prompt_few_kernel(PromptParams p) {
+  constexpr int kTile = kFewKeys * TKV_D * 2;
+  extern __shared__ __attribute__((aligned(1024))) char few_lds[];  // [wave][2][K, V tile]
+  const int lane = threadIdx.x % 64, half = lane / 32, col = lane % 32;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
+  const int h = blockIdx.x % p.hkv;
+  const Item it = find_item(p, blockIdx.x / p.hkv);
+  const PromptSeq sq = p.seq[it.b];
+  const int rows = sq.q_len * p.group, ahead = sq.k_len - sq.q_len, pieces = p.pieces[it.b];
+  const int all_tiles = (sq.k_len + kFewKeys - 1) / kFewKeys;
+  const int share = it.piece * kFewWaves + wave, shares = pieces * kFewWaves;
+  const int t0 = (int)((int64_t)all_tiles * share / shares), t1 = (int)((int64_t)all_tiles * (share + 1) / shares);
+  const int row_ok = min(col, rows - 1), token = row_ok / p.group, head = row_ok - token * p.group;
+  const int limit = p.causal ? token + ahead : sq.k_len - 1;
+  const int limit_low = p.causal ? ahead : sq.k_len - 1;
+
+  uint32_t k_off[8], v_off[8];
+#pragma unroll
+  for (int j = 0; j < 8; ++j) {
+    const int r = 4 * j + lane / 16, place = lane % 16;
+    k_off[j] = (uint32_t)(r * p.k_st * 2) + 16u * (uint32_t)(place ^ (r & 15));
+    v_off[j] = (uint32_t)(r * p.v_st * 2) + 16u * (uint32_t)(place ^ (((r & 3) << 2) | ((r >> 2) & 3)));
+  }
+  const char* k_base = (const char*)p.k + ((int64_t)sq.k_start * p.k_st + (int64_t)h * p.k_sh) * 2;
+  const char* v_base = (const char*)p.v + ((int64_t)sq.k_start * p.v_st + (int64_t)h * p.v_sh) * 2;
+  lds_char* const ring = (lds_char*)few_lds + wave * 4 * kTile;
+  const uint32_t ring0 = (uint32_t)(uintptr_t)ring;
+  auto stage = [&](int t) {
+    t = min(t, t1 - 1);  // (as many loads in every step)
+    const int left = min(kFewKeys, sq.k_len - t * kFewKeys);  // rows behind the sequence's last read as zeros
+    const auto kr = __builtin_amdgcn_make_buffer_rsrc((void*)(k_base + (int64_t)t * kFewKeys * p.k_st * 2), 0, (int)((left - 1) * p.k_st * 2 + TKV_D * 2), 0x00020000);
+    const auto vr = __builtin_amdgcn_make_buffer_rsrc((void*)(v_base + (int64_t)t * kFewKeys * p.v_st * 2), 0, (int)((left - 1) * p.v_st * 2 + TKV_D * 2), 0x00020000);
+    return [=](int buf) {
+      const uint32_t to = ring0 + (uint32_t)(buf * 2 * kTile);
+#pragma unroll
+      for (int j = 0; j < 8; ++j) to_lds(kr, to + 1024 * j, k_off[j]);
+#pragma unroll
+      for (int j = 0; j < 8; ++j) to_lds(vr, to + kTile + 1024 * j, v_off[j]);
+    };
+  };
+  if (t0 < t1) stage(t0)(0);
+  uintx4 qf[8];
+  {
+    const T* q = (const T*)p.q + ((int64_t)(sq.q_start + token) * p.q_st + (int64_t)(h * p.group + head) * p.q_sh + 8 * half);
+#pragma unroll
+    for (int kk = 0; kk < 8; ++kk) qf[kk] = *(const uintx4*)(q + 16 * kk);
+  }
+  lds_char* ka[8];
+  lds_char* va[8];
+#pragma unroll
+  for (int kk = 0; kk < 8; ++kk) ka[kk] = ring + (col * 256 + 16 * ((2 * kk + half) ^ (col & 15)));
+  {
+    const int l16 = lane % 16, right = (lane / 16) % 2;
+#pragma unroll
+    for (int dt = 0; dt < 4; ++dt)
+#pragma unroll
+      for (int s = 0; s < 2; ++s) {
+        const int key = 8 * s + 4 * half + l16 / 4;
+        const int place = (4 * dt + 2 * right + (l16 % 4) / 2) ^ (((key & 3) << 2) | ((key >> 2) & 3));
+        va[2 * dt + s] = ring + (kTile + key * 256 + 16 * place + 8 * (l16 % 2));
+      }
+  }
+  floatx16 o[4];
+#pragma unroll
+  for (int dt = 0; dt < 4; ++dt)
+#pragma unroll
+    for (int i = 0; i < 16; ++i) o[dt][i] = 0.f;
+  float ref = kNone, sum = 0.f;
+#pragma unroll
+  for (int kk = 0; kk < 8; ++kk) asm volatile("" : "+v"(qf[kk]));  // (waited for here, not in the loop)
+
+  for (int t = t0; t < t1; ++t) {
+    const int at = ((t - t0) & 1) * 2 * kTile, key0 = t * kFewKeys;
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // (the other buffer's reads are done)
+    stage(t + 1)((t + 1 - t0) & 1);
+    asm volatile("s_waitcnt vmcnt(16)" ::: "memory");
+    floatx16 s;
+#pragma unroll
+    for (int i = 0; i < 16; ++i) s[i] = 0.f;
+#pragma unroll
+    for (int kk = 0; kk < 8; ++kk) s = mfma32<T>(lds_read16(ka[kk] + at), qf[kk], s);
+    if (key0 + kFewKeys - 1 > limit_low || key0 + kFewKeys > sq.k_len) {
+#pragma unroll
+      for (int i = 0; i < 16; ++i) s[i] = key0 + 8 * (i / 4) + 4 * half + i % 4 <= limit ? s[i] : -INFINITY;
+    }
+    float top = s[0];
+#pragma unroll
+    for (int i = 1; i < 16; ++i) top = fmaxf(top, s[i]);
+    top = fmaxf(top, other_half(top, half)) * p.scale2;
+    if (__builtin_amdgcn_ballot_w64(top > ref + 8.f) != 0) {
+      const float next = fmaxf(ref, top), shrink = __builtin_amdgcn_exp2f(ref - next);
+      ref = next;
+      sum *= shrink;
+#pragma unroll
+      for (int dt = 0; dt < 4; ++dt) o[dt] *= shrink;
+    }
+    const float less = kShift - ref;
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+      s[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[i], p.scale2, less));
+      sum += s[i];
+    }
+    uintx4 pf[2];
+    pf[0] = pack8<T>(__builtin_shufflevector(s, s, 0, 1, 2, 3, 4, 5, 6, 7));
+    pf[1] = pack8<T>(__builtin_shufflevector(s, s, 8, 9, 10, 11, 12, 13, 14, 15));
+#pragma unroll
+    for (int ks = 0; ks < 2; ++ks)
+#pragma unroll
+      for (int dt = 0; dt < 4; ++dt) {
+        const uintx2 lo = lds_read_tr(va[2 * dt] + at + 4096 * ks), hi = lds_read_tr(va[2 * dt + 1] + at + 4096 * ks);
+        o[dt] = mfma32<T>(__builtin_shufflevector(lo, hi, 0, 1, 2, 3), pf[ks], o[dt]);
+      }
+  }
+  sum += other_half(sum, half);
+  asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");  // no load may land after the ring is used otherwise
+  __syncthreads();
+
+  // the waves joined: everyone's sums and references into LDS, then wave w works out channels 32 w to 32 w + 31
+  float* const ml_s = (float*)few_lds;                              // [wave][32][2]
+  float* const o_s = (float*)few_lds + kFewWaves * kFew * 2;        // [wave][32 rows][132]
+  constexpr int kRowStride = TKV_D + 4;
+  if (half == 0) {
+    ml_s[(wave * kFew + col) * 2] = ref;
+    ml_s[(wave * kFew + col) * 2 + 1] = sum;
+  }
+#pragma unroll
+  for (int dt = 0; dt < 4; ++dt)
+#pragma unroll
+    for (int y = 0; y < 4; ++y)
+      *(floatx4*)(o_s + (wave * kFew + col) * kRowStride + 32 * dt + 8 * y + 4 * half) = (floatx4){o[dt][4 * y], o[dt][4 * y + 1], o[dt][4 * y + 2], o[dt][4 * y + 3]};
+  __syncthreads();
+  if (col >= rows) return;
+  float m[kFewWaves], top = kNone, total = 0.f;
+#pragma unroll
+  for (int w = 0; w < kFewWaves; ++w) top = fmaxf(top, m[w] = ml_s[(w * kFew + col) * 2]);
+#pragma unroll
+  for (int w = 0; w < kFewWaves; ++w) {
+    m[w] = __builtin_amdgcn_exp2f(m[w] - top);
+    total = __builtin_fmaf(ml_s[(w * kFew + col) * 2 + 1], m[w], total);
+  }
+  floatx4 x[4];  // row col, channels 32 wave + 16 half + 0 .. 15
+  const int c0 = 32 * wave + 16 * half;
+#pragma unroll
+  for (int y = 0; y < 4; ++y) {
+    x[y] = (floatx4){0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int w = 0; w < kFewWaves; ++w) x[y] += *(const floatx4*)(o_s + (w * kFew + col) * kRowStride + c0 + 4 * y) * m[w];
+  }
+  if (p.first_part[it.b] >= 0) {
+    const size_t part = (size_t)p.first_part[it.b] + (size_t)it.piece * p.hkv + h;
+    if (wave == 0 && half == 0) *(float2*)(p.ml + (part * kFew + col) * 2) = make_float2(top, total);
+    float* to = p.parts + (part * kFew + col) * TKV_D + c0;
+#pragma unroll
+    for (int y = 0; y < 4; ++y) *(floatx4*)(to + 4 * y) = x[y];
+    return;
+  }
+  const float inv = total == 0.f ? 0.f : 1.f / total;  // (no key: zeros)
+  T* to = (T*)p.out + ((int64_t)(sq.q_start + token) * p.o_st + (int64_t)(h * p.group + head) * p.o_sh) + c0;
+#pragma unroll
+  for (int y = 0; y < 2; ++y)
+    *(uintx4*)(to + 8 * y) = pack8<T>(__builtin_shufflevector(x[2 * y] * inv, x[2 * y + 1] * inv, 0, 1, 2, 3, 4, 5, 6, 7));
+  if (p.lse && wave == 0 && half == 0)
+    p.lse[(int64_t)(sq.q_start + token) * p.hq + h * p.group + head] =
+        total == 0.f ? -INFINITY : (top - kShift + __builtin_amdgcn_logf(total)) * 0.69314718055994531f;
+}
+
+// Joins the pieces of the split rows: a workgroup per row, every wave a quarter of the pieces, a lane two channels.
 template <typename T>
 __global__ __launch_bounds__(256) void prompt_merge_kernel(PromptParams p) {
+  __shared__ float acc_s[4][TKV_D], l_s[4], m_s[4];
   const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
-  const int h = blockIdx.x % p.hkv;
-  // (the grid runs over tiles: the items of pieces 0)
-  int tile = blockIdx.x / p.hkv, b = 0;
-  for (; b < p.batch; ++b) {
-    if (p.first_part[b] < 0) continue;
-    const int tiles = (p.seq[b].q_len * p.group + kRows - 1) / kRows;
-    if (tile < tiles) break;
-    tile -= tiles;
-  }
-  if (b >= p.batch) return;
-  const int r = 4 * blockIdx.y + wave, row = tile * kRows + r;
-  if (row >= p.seq[b].q_len * p.group) return;
+  const int h = blockIdx.x % p.hkv, at = blockIdx.x / p.hkv;
+  // the last sequence that begins at or before the row (those that are not split share their successor's beginning)
+  const bool before = lane < p.batch && p.first_row[min(lane, p.batch - 1)] <= at;
+  const int b = __builtin_amdgcn_readfirstlane(__builtin_popcountll(__builtin_amdgcn_ballot_w64(before)) - 1);
+  const int row = at - p.first_row[b], tile = row / p.tile_rows, r = row - tile * p.tile_rows;
   const int token = row / p.group, head = row - token * p.group, pieces = p.pieces[b];
-  const size_t part0 = (size_t)p.first_part[b] + (size_t)tile * pieces * p.hkv + h;
-  const float* ml = p.parts + (size_t)kMaxParts * kRows * TKV_D;
+  const size_t slot0 = ((size_t)p.first_part[b] + (size_t)tile * pieces * p.hkv + h) * p.tile_rows + r;
+  const size_t step = (size_t)p.hkv * p.tile_rows;
   float m = kNone, l = 0.f;
-  if (lane < pieces) {
-    const float2 x = *(const float2*)(ml + ((part0 + (size_t)lane * p.hkv) * kRows + r) * 2);
-    m = x.x, l = x.y;
-  }
-  const float top = tkv::over_wave(m, tkv::MaxOf{});
-  const float w = __builtin_amdgcn_exp2f(m - top);
-  const float total = tkv::over_wave(l * w, tkv::SumOf{});
   float2 acc = make_float2(0.f, 0.f);
-  for (int i = 0; i < pieces; ++i) {
-    const float li = __shfl(l, i, 64), wi = __shfl(w, i, 64);
-    if (li == 0.f) continue;
-    const float2 x = *(const float2*)(p.parts + ((part0 + (size_t)i * p.hkv) * kRows + r) * TKV_D + 2 * lane);
-    acc.x = __builtin_fmaf(x.x, wi, acc.x);
-    acc.y = __builtin_fmaf(x.y, wi, acc.y);
+  // (requests of eight pieces at a time, absent ones those of the first with a weight of zero)
+  for (int i0 = wave; i0 < pieces; i0 += 32) {
+    float2 st[8], v[8];
+#pragma unroll
+    for (int y = 0; y < 8; ++y) {
+      const size_t s = slot0 + (i0 + 4 * y < pieces ? i0 + 4 * y : 0) * step;
+      st[y] = *(const float2*)(p.ml + s * 2);
+      v[y] = *(const float2*)(p.parts + s * TKV_D + 2 * lane);
+    }
+    float top = m;
+#pragma unroll
+    for (int y = 0; y < 8; ++y) top = fmaxf(top, st[y].x);
+    const float shrink = __builtin_amdgcn_exp2f(m - top);
+    m = top;
+    l *= shrink;
+    acc.x *= shrink;
+    acc.y *= shrink;
+#pragma unroll
+    for (int y = 0; y < 8; ++y) {
+      const float w = i0 + 4 * y < pieces ? __builtin_amdgcn_exp2f(st[y].x - m) : 0.f;
+      l = __builtin_fmaf(st[y].y, w, l);
+      acc.x = __builtin_fmaf(v[y].x, w, acc.x);
+      acc.y = __builtin_fmaf(v[y].y, w, acc.y);
+    }
   }
-  const float inv = total == 0.f ? 0.f : 1.f / total;
+  *(float2*)(acc_s[wave] + 2 * lane) = acc;
+  if (lane == 0) l_s[wave] = l, m_s[wave] = m;
+  __syncthreads();
+  if (threadIdx.x >= TKV_D) return;
+  const int c = threadIdx.x;
+  const float top = fmaxf(fmaxf(m_s[0], m_s[1]), fmaxf(m_s[2], m_s[3]));
+  float total = 0.f, v = 0.f;
+#pragma unroll
+  for (int w = 0; w < 4; ++w) {
+    const float f = __builtin_amdgcn_exp2f(m_s[w] - top);
+    total = __builtin_fmaf(l_s[w], f, total);
+    v = __builtin_fmaf(acc_s[w][c], f, v);
+  }
   T* to = (T*)p.out + ((int64_t)(p.seq[b].q_start + token) * p.o_st + (int64_t)(h * p.group + head) * p.o_sh);
-  typedef T T2 __attribute__((ext_vector_type(2)));
-  typedef float floatx2 __attribute__((ext_vector_type(2)));
-  *(T2*)(to + 2 * lane) = __builtin_convertvector((floatx2){acc.x * inv, acc.y * inv}, T2);
-  if (p.lse && lane == 0)
+  to[c] = (T)(total == 0.f ? 0.f : v / total);
+  if (p.lse && c == 0)
     p.lse[(int64_t)(p.seq[b].q_start + token) * p.hq + h * p.group + head] =
         total == 0.f ? -INFINITY : (top - kShift + __builtin_amdgcn_logf(total)) * 0.69314718055994531f;
+}
+
+template <typename T>
+int32_t launch_prompt(const PromptParams& p, bool few, int32_t items, int32_t split_rows, hipStream_t s) {
+  const dim3 grid((uint32_t)items * (uint32_t)p.hkv);
+  if (few) {
+    constexpr int lds = kFewWaves * 4 * kFewKeys * TKV_D * 2;
+    static_assert(lds <= 160 * 1024 && kFewWaves * kFew * (TKV_D + 4 + 2) * 4 <= lds, "LDS of one compute unit");
+    static const bool lds_ok = hipFuncSetAttribute(reinterpret_cast<const void*>(&prompt_few_kernel<T>),
+                                                   hipFuncAttributeMaxDynamicSharedMemorySize, lds) == hipSuccess;
+    if (!lds_ok) return TKV_E_HIP;
+    TKV_LAUNCH(prompt_few_kernel<T>, grid, 64 * kFewWaves, lds, s, p);
+  } else {
+    TKV_LAUNCH(prompt_attn_kernel<T>, grid, 64 * kWaves, 0, s, p);
+  }
+  if (split_rows) TKV_LAUNCH(prompt_merge_kernel<T>, dim3((uint32_t)split_rows * (uint32_t)p.hkv), 256, 0, s, p);
+  return TKV_OK;
 }
 
 int32_t check_prompt_desc(const tkv_prompt_desc* d) {
@@ -376,8 +643,8 @@ extern "C" int32_t tkv_prompt_attn(const tkv_prompt_desc* d, const void* q, cons
   }
   if (tiles == 0) return TKV_OK;
   if (!q || !out || (any_keys && (!k || !v))) return TKV_E_INVAL;
-  if (tiles * 64 * d->n_kv_heads > 0x7FFFFFFF) return TKV_E_UNSUPPORTED;
-  p.q = q; p.k = k; p.v = v; p.out = out; p.lse = lse; p.parts = (float*)workspace;
+  if (tiles * 2 * d->n_kv_heads > 0x7FFFFFFF) return TKV_E_UNSUPPORTED;
+  p.q = q; p.k = k; p.v = v; p.out = out; p.lse = lse;
   p.q_st = d->q_stride[0]; p.q_sh = d->q_stride[1];
   p.k_st = d->k_stride[0]; p.k_sh = d->k_stride[1];
   p.v_st = d->v_stride[0]; p.v_sh = d->v_stride[1];
@@ -385,42 +652,44 @@ extern "C" int32_t tkv_prompt_attn(const tkv_prompt_desc* d, const void* q, cons
   p.hq = d->n_q_heads; p.hkv = d->n_kv_heads; p.batch = d->batch; p.causal = d->causal;
   p.scale2 = sm_scale * 1.4426950408889634f;
 
-  // Few row tiles: their keys are split into pieces so that about two workgroups per compute unit have work.
-  auto key_tiles = [&](int b) { return (k_len_host[b] + kKeys - 1) / kKeys; };
-  auto row_tiles = [&](int b) { return (q_len_host[b] * p.group + kRows - 1) / kRows; };
-  int64_t per_piece = 0;
-  if (tiles * d->n_kv_heads < 384) {
-    int64_t work = 0;
-    for (int b = 0; b < d->batch; ++b) work += (int64_t)row_tiles(b) * key_tiles(b) * d->n_kv_heads;
-    per_piece = work / 512 < 4 ? 4 : work / 512;
+  // Few row tiles: their keys are split into pieces, as many as give every compute unit one workgroup (a workgroup of either
+  // kernel takes most of its compute unit's registers or LDS), of at least four tiles of keys (per wave, where the waves take their own).
+  bool few = true;
+  for (int b = 0; b < d->batch; ++b) few = few && (int64_t)q_len_host[b] * p.group <= kFew;
+  p.tile_rows = few ? kFew : kRows;
+  const int keys = few ? kFewKeys * kFewWaves : kKeys;
+  auto key_tiles = [&](int b) { return (k_len_host[b] + keys - 1) / keys; };
+  auto row_tiles = [&](int b) { return (q_len_host[b] * p.group + p.tile_rows - 1) / p.tile_rows; };
+  int64_t work = 0, whole = 0;
+  for (int b = 0; b < d->batch; ++b) {
+    work += (int64_t)row_tiles(b) * key_tiles(b) * d->n_kv_heads;
+    whole += (int64_t)row_tiles(b) * d->n_kv_heads;
   }
-  int32_t items = 0, parts = 0, split_tiles = 0;
-  for (;; per_piece *= 2) {
-    items = parts = split_tiles = 0;
+  double per_piece = whole < kWorkgroups ? (double)work / kWorkgroups : 0;
+  if (per_piece > 0 && per_piece < 4) per_piece = 4;
+  int32_t items = 0, parts = 0, split_rows = 0;
+  for (;; per_piece *= 1.05) {
+    items = parts = split_rows = 0;
     for (int b = 0; b < d->batch; ++b) {
       p.seq[b] = {q_start_host[b], q_len_host[b], k_start_host[b], k_len_host[b]};
-      int64_t pieces = per_piece ? (key_tiles(b) + per_piece - 1) / per_piece : 1;
-      pieces = pieces < 1 ? 1 : pieces > 64 ? 64 : pieces;
+      int64_t pieces = per_piece > 0 ? (int64_t)((double)key_tiles(b) / per_piece) : 1;
+      if (per_piece > 0 && (double)pieces * per_piece < key_tiles(b)) ++pieces;
+      pieces = pieces < 1 ? 1 : pieces;
       p.pieces[b] = (int32_t)pieces;
       p.first_item[b] = items;
       p.first_part[b] = -1;
+      p.first_row[b] = split_rows;
       items += row_tiles(b) * p.pieces[b];
       if (pieces > 1 && row_tiles(b) > 0) {
         p.first_part[b] = parts;
         parts += row_tiles(b) * p.pieces[b] * d->n_kv_heads;
-        split_tiles += row_tiles(b);
+        split_rows += q_len_host[b] * p.group;
       }
     }
-    if (parts <= kMaxParts) break;
+    if (per_piece == 0 || (int64_t)items * d->n_kv_heads <= kWorkgroups) break;  // (at the latest with one piece each)
   }
+  p.parts = (float*)workspace;
+  p.ml = p.parts + (size_t)kMaxParts * kRows * TKV_D;
   const auto s = (hipStream_t)stream;
-  const dim3 grid((uint32_t)items * (uint32_t)d->n_kv_heads), merge((uint32_t)split_tiles * (uint32_t)d->n_kv_heads, kRows / 4);
-  if (d->dtype == TKV_F16) {
-    TKV_LAUNCH(prompt_attn_kernel<_Float16>, grid, 256, 0, s, p);
-    if (split_tiles) TKV_LAUNCH(prompt_merge_kernel<_Float16>, merge, 256, 0, s, p);
-  } else {
-    TKV_LAUNCH(prompt_attn_kernel<__bf16>, grid, 256, 0, s, p);
-    if (split_tiles) TKV_LAUNCH(prompt_merge_kernel<__bf16>, merge, 256, 0, s, p);
-  }
-  return TKV_OK;
+  return d->dtype == TKV_F16 ? launch_prompt<_Float16>(p, few, items, split_rows, s) : launch_prompt<__bf16>(p, few, items, split_rows, s);
 }

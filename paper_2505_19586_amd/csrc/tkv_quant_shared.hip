@@ -27,6 +27,7 @@ typedef uint32_t uintx4 __attribute__((ext_vector_type(4)));
 typedef uint32_t uintx2 __attribute__((ext_vector_type(2)));
 typedef short shortx4 __attribute__((ext_vector_type(4)));
 typedef __attribute__((address_space(3))) char lds_char;
+typedef lds_char* lds_at;  // (pointers, not numbers: so that constant offsets go into the instructions)
 
 constexpr int kWaves = 8;
 constexpr int kSlots = 3;            // blocks of a wave on their way or in use
@@ -90,10 +91,11 @@ __device__ inline void codes(const uint32_t* w, uint32_t or_in, half2_t (&c)[4])
   }
 }
 
-__device__ inline uintx4 lds_read16(uint32_t at) { return *(__attribute__((address_space(3))) uintx4*)(lds_char*)(uintptr_t)at; }
-__device__ inline void lds_write16(uint32_t at, uintx4 v) { *(__attribute__((address_space(3))) uintx4*)(lds_char*)(uintptr_t)at = v; }
-__device__ inline uintx2 lds_read_tr(uint32_t at) {
-  return __builtin_bit_cast(uintx2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) shortx4*)(lds_char*)(uintptr_t)at));
+__device__ inline uintx4 lds_read16(lds_at at) { return *(__attribute__((address_space(3))) uintx4*)at; }
+__device__ inline void lds_write16(lds_at at, uintx4 v) { *(__attribute__((address_space(3))) uintx4*)at = v; }
+__device__ inline uint32_t lds_word(lds_at at) { return *(__attribute__((address_space(3))) uint32_t*)at; }
+__device__ inline uintx2 lds_read_tr(lds_at at) {
+  return __builtin_bit_cast(uintx2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) shortx4*)at));
 }
 // 16 bytes per lane straight to LDS, in lane order from `to` (uniform) on; the caller waits (vmcnt).  By hand, so that the compiler
 // makes no LDS read wait for loads of other slots.  (m0 is used by nothing else here.)
@@ -125,14 +127,14 @@ __device__ inline void attend(const SharedParams& p, const SharedCache& c, int s
                               const uint8_t* order, int row0, int rows, int64_t slot0) {
   constexpr int G = 32 * GS, CB = code_bytes<BITS>(), SB = slot_bytes<BITS>();
   extern __shared__ __attribute__((aligned(1024))) char lds[];
-  const uint32_t lds0 = (uint32_t)(uintptr_t)(lds_char*)lds;
+  const lds_at lds0 = (lds_at)lds;
   const int lane = threadIdx.x % 64, kb = lane / 16, col = lane % 16;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
-  constexpr uint32_t kRing = kWaves * kSlots * SB;
-  constexpr uint32_t kStats = lds_bytes<BITS, MAXQ>() - kWaves * 16 * MAXQ * 8;
+  constexpr int kRing = kWaves * kSlots * SB;
+  constexpr int kStats = lds_bytes<BITS, MAXQ>() - kWaves * 16 * MAXQ * 8;
   constexpr int SPAN = span_groups<BITS>(), C0 = code_zero<BITS>();
-  const uint32_t ring = lds0 + (uint32_t)(wave * kSlots * SB), q_at = lds0 + kRing, stats = lds0 + kStats;
-  const uint32_t terms = q_at + MAXQ * 4096 + (uint32_t)(wave * SPAN * NQ * 64);  // [group][tile][16 columns] float32
+  const lds_at ring = lds0 + wave * kSlots * SB, q_at = lds0 + kRing, stats = lds0 + kStats;
+  const lds_at terms = q_at + MAXQ * 4096 + wave * SPAN * NQ * 64;  // [group][tile][16 columns] float32
 
   // blocks of the segment: quantized ones, then the ring's rows in pieces of 32; this wave's share of the chunk's
   const int nq = tkv::n_quantized(n, c.residual, G), coded = nq / 32, blocks = coded + (n - nq + 31) / 32;
@@ -156,7 +158,7 @@ __device__ inline void attend(const SharedParams& p, const SharedCache& c, int s
     }
   }
   auto stage = [&](int slot, int j) {
-    const uint32_t to = ring + (uint32_t)(slot * SB);
+    const uint32_t to = (uint32_t)(uintptr_t)(ring + slot * SB);
     const uint32_t mine = BITS == 1 ? 16u * (uint32_t)(lane % 32) : 16u * (uint32_t)lane;
     const int64_t at = (int64_t)j * (512 * BITS);
 #pragma unroll
@@ -181,7 +183,7 @@ __device__ inline void attend(const SharedParams& p, const SharedCache& c, int s
       const uint32_t* from = (const uint32_t*)(p.q + ((int64_t)b * p.hq + h * p.group + g) * TKV_D + 32 * (y % 4) + 8 * kb);
       v = (uintx4){from[0], from[1], from[2], from[3]};
     }
-    lds_write16(q_at + (uint32_t)(y * 1024 + 16 * lane), v);
+    lds_write16(q_at + y * 1024 + 16 * lane, v);
   }
   __syncthreads();
 
@@ -252,73 +254,68 @@ __device__ inline void attend(const SharedParams& p, const SharedCache& c, int s
       floatx4 v = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
       for (int m = 0; m < 4; ++m) {
-        const uintx4 q = lds_read16(q_at + (uint32_t)((4 * t + m) * 1024 + 16 * lane));
+        const uintx4 q = lds_read16(q_at + 16 * lane + (4 * t + m) * 1024);
         v = mfma(z[m], q, v);
         if constexpr (C0 > 0) v = mfma(sc[m], q, v);
       }
       if (4 * kb < SPAN) {
 #pragma unroll
         for (int i = 0; i < 4; ++i)
-          *(__attribute__((address_space(3))) float*)(lds_char*)(uintptr_t)(terms + (uint32_t)(((4 * kb + i) * NQ + t) * 64 + 4 * col)) = v[i] * p.scale2;
+          *(__attribute__((address_space(3))) float*)(terms + ((4 * kb + i) * NQ + t) * 64 + 4 * col) = v[i] * p.scale2;
       }
     }
   };
 
+  auto words = [&](lds_at from, uint32_t* w) {
+    if constexpr (BITS == 1) {
+      w[0] = lds_word(from + 4 * lane);
+      w[1] = lds_word(from + 4 * lane + 256);
+    } else {
+      const uintx4 a = lds_read16(from + 16 * lane);
+      w[0] = a.x, w[1] = a.y, w[2] = a.z, w[3] = a.w;
+      if constexpr (BITS == 4) {
+        const uintx4 b = lds_read16(from + 16 * lane + 1024);
+        w[4] = b.x, w[5] = b.y, w[6] = b.z, w[7] = b.w;
+      }
+    }
+  };
+  // A block's LDS reads go out a stage ahead of their use: the keys' codes and the first channels' scalers and queries during the
+  // products of the block before, those of the next 32 channels during each quarter of the logits, the values' before the weights.
+  uint32_t kw[8];
+  uintx4 ks[2], q[2][NQ];
+  auto read_channels = [&](int m, lds_at at) {  // 32 m on
+    ks[m % 2] = lds_read16(at + 16 * kb + (2 * CB + 64 * m));
+#pragma unroll
+    for (int t = 0; t < NQ; ++t) q[m % 2][t] = lds_read16(q_at + 16 * lane + (4 * t + m) * 1024);
+  };
+  if (b0 < c1) {
+    asm volatile("s_waitcnt vmcnt(%0)" ::"n"(kLoads) : "memory");
+    words(ring, kw);
+    read_channels(0, ring);
+  }
   int slot = 0, span_end = b0;
-  uint32_t term_at = terms;
+  lds_at term_at = terms;
   for (int j = b0; j < c1; ++j) {
     if (j >= span_end) {
       work_out_terms(j);
       span_end = (j / GS + SPAN) * GS;
       term_at = terms;
     }
-    // (the next block but one goes where the previous block was; its reads are done)
-    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+    // (the next block but one goes where the previous block was, whose reads are done)
     stage(slot == 0 ? 2 : slot - 1, min(j + 2, c1 - 1));
-    asm volatile("s_waitcnt vmcnt(%0)" ::"n"(2 * kLoads) : "memory");
-    const uint32_t at = ring + (uint32_t)(slot * SB);
+    const lds_at at = ring + slot * SB;
     slot = slot == kSlots - 1 ? 0 : slot + 1;
-    auto words = [&](uint32_t from, uint32_t* w) {
-      if constexpr (BITS == 1) {
-        w[0] = *(__attribute__((address_space(3))) uint32_t*)(lds_char*)(uintptr_t)(from + 4 * lane);
-        w[1] = *(__attribute__((address_space(3))) uint32_t*)(lds_char*)(uintptr_t)(from + 256 + 4 * lane);
-      } else {
-        const uintx4 a = lds_read16(from + 16 * lane);
-        w[0] = a.x, w[1] = a.y, w[2] = a.z, w[3] = a.w;
-        if constexpr (BITS == 4) {
-          const uintx4 b = lds_read16(from + 1024 + 16 * lane);
-          w[4] = b.x, w[5] = b.y, w[6] = b.z, w[7] = b.w;
-        }
-      }
-    };
-    // every LDS read of the keys' side is under way before the first is used
-    const uint32_t meta_at = at + 2 * CB;
-    uint32_t kw[8], vw[8];
-    uintx4 ks[4];
     float base[NQ];
-    words(at, kw);
 #pragma unroll
-    for (int m = 0; m < 4; ++m) ks[m] = lds_read16(meta_at + 64 * m + 16 * kb);
-    constexpr int AHEAD = NQ < 4 ? 1 : 0;  // (no registers left for it with four tiles)
-    uintx4 q[2][NQ];
-    if constexpr (AHEAD) {
-#pragma unroll
-      for (int t = 0; t < NQ; ++t) q[0][t] = lds_read16(q_at + (uint32_t)(4 * t * 1024 + 16 * lane));
-    }
-#pragma unroll
-    for (int t = 0; t < NQ; ++t) base[t] = *(__attribute__((address_space(3))) float*)(lds_char*)(uintptr_t)(term_at + 64 * t + 4 * col);
+    for (int t = 0; t < NQ; ++t) base[t] = __uint_as_float(lds_word(term_at + 4 * col + 64 * t));
     if (GS == 1 || j % 2 == 1) term_at += NQ * 64;
-    __builtin_amdgcn_sched_barrier(0);
     floatx4 s[2][NQ];
 #pragma unroll
     for (int t = 0; t < NQ; ++t) s[0][t] = s[1][t] = (floatx4){0.f, 0.f, 0.f, 0.f};
     auto keys = [&](auto M) {  // channels 32 m on
       constexpr int m = decltype(M)::value;
-      constexpr int n = m + AHEAD;
-      if constexpr (n < 4) {
-#pragma unroll
-        for (int t = 0; t < NQ; ++t) q[n % 2][t] = lds_read16(q_at + (uint32_t)((4 * t + n) * 1024 + 16 * lane));
-      }
+      __builtin_amdgcn_sched_barrier(0);
+      if constexpr (m < 3) read_channels(m + 1, at);
       half2_t code0[4], code1[4];
       codes<BITS, m, C0>(kw, or_in, code0);
       codes<BITS, 4 + m, C0>(kw, or_in, code1);
@@ -327,7 +324,7 @@ __device__ inline void attend(const SharedParams& p, const SharedCache& c, int s
         uintx4 k0, k1;
 #pragma unroll
         for (int y = 0; y < 4; ++y) {
-          uint32_t sw = ks[m][y];
+          uint32_t sw = ks[m % 2][y];
           if constexpr (BITS == 4) {
             const uint32_t high = sw & 0xFFF8FFF8u;
             sw = part == 0 ? high : as_word(as_half2(sw) - as_half2(high));
@@ -347,16 +344,21 @@ __device__ inline void attend(const SharedParams& p, const SharedCache& c, int s
     keys(std::integral_constant<int, 2>{});
     keys(std::integral_constant<int, 3>{});
     constexpr int U = 128 / G;
+    uint32_t vw[8];
     uintx4 vs[U], vz[U];
     words(at + CB, vw);
 #pragma unroll
     for (int u = 0; u < U; ++u) {
-      vs[u] = lds_read16(meta_at + 512 + 64 * u + 16 * kb);
-      vz[u] = lds_read16(meta_at + 768 + 64 * u + 16 * kb);
+      vs[u] = lds_read16(at + 16 * kb + (2 * CB + 512 + 64 * u));
+      vz[u] = lds_read16(at + 16 * kb + (2 * CB + 768 + 64 * u));
     }
     __builtin_amdgcn_sched_barrier(0);
     uintx4 w[NQ];
     soften(s, base, w);
+    asm volatile("s_waitcnt vmcnt(%0)" ::"n"(kLoads) : "memory");  // block j + 1 is there
+    words(ring + slot * SB, kw);
+    read_channels(0, ring + slot * SB);
+    __builtin_amdgcn_sched_barrier(0);
     auto values = [&](auto X) {  // channels 16 x on
       constexpr int x = decltype(X)::value, u = x * 16 / G;
       half2_t cv[4];
@@ -378,6 +380,7 @@ __device__ inline void attend(const SharedParams& p, const SharedCache& c, int s
     values(std::integral_constant<int, 5>{});
     values(std::integral_constant<int, 6>{});
     values(std::integral_constant<int, 7>{});
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // (long there: this block's last reads, before its slot is given away)
   }
   asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");  // no load may land after the ring is used otherwise
 
@@ -397,14 +400,14 @@ __device__ inline void attend(const SharedParams& p, const SharedCache& c, int s
     for (int x = 0; x < 8; ++x) kk[x] = __builtin_amdgcn_raw_buffer_load_b128(kr, (token + 4 * (x / 4)) * 256 + 64 * (x % 4) + 16 * kb, 0, 0);
     asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
 #pragma unroll
-    for (int y = 0; y < 8; ++y) lds_write16(ring + 1024 * y + 16 * lane, vv[y]);
+    for (int y = 0; y < 8; ++y) lds_write16(ring + 16 * lane + 1024 * y, vv[y]);
     floatx4 s[2][NQ];
 #pragma unroll
     for (int t = 0; t < NQ; ++t) {
       s[0][t] = s[1][t] = (floatx4){0.f, 0.f, 0.f, 0.f};
 #pragma unroll
       for (int m = 0; m < 4; ++m) {
-        const uintx4 q = lds_read16(q_at + (uint32_t)((4 * t + m) * 1024 + 16 * lane));
+        const uintx4 q = lds_read16(q_at + 16 * lane + (4 * t + m) * 1024);
         s[0][t] = mfma(kk[m], q, s[0][t]);
         s[1][t] = mfma(kk[4 + m], q, s[1][t]);
       }
@@ -420,7 +423,7 @@ __device__ inline void attend(const SharedParams& p, const SharedCache& c, int s
 #pragma unroll
     for (int x = 0; x < 8; ++x) {
       // tokens 8 kb to 8 kb + 7 of channel 16 x + col: two blocks of four rows, transposed
-      const uint32_t from = ring + (uint32_t)((8 * kb + col / 4) * 256 + 32 * x + 8 * (col % 4));
+      const lds_at from = ring + ((8 * kb + col / 4) * 256 + 8 * (col % 4)) + 32 * x;
       const uintx2 lo = lds_read_tr(from), hi = lds_read_tr(from + 1024);
       const uintx4 v = __builtin_shufflevector(lo, hi, 0, 1, 2, 3);
 #pragma unroll
@@ -434,7 +437,7 @@ __device__ inline void attend(const SharedParams& p, const SharedCache& c, int s
   for (int t = 0; t < NQ; ++t) {
     const float total = tkv::over_rows(sum[t], tkv::SumOf{});
     if (kb == 0) {
-      auto* st = (__attribute__((address_space(3))) float*)(lds_char*)(uintptr_t)(stats + (uint32_t)((t * kWaves + wave) * 16 + col) * 8);
+      auto* st = (__attribute__((address_space(3))) float*)(stats + ((t * kWaves + wave) * 16 + col) * 8);
       st[0] = ref[t];
       st[1] = total;
     }
@@ -443,7 +446,7 @@ __device__ inline void attend(const SharedParams& p, const SharedCache& c, int s
 #pragma unroll
   for (int t = 0; t < NQ; ++t) {
     float m[kWaves], l = 0.f, top = kNone;
-    const auto* st = (const __attribute__((address_space(3))) float*)(lds_char*)(uintptr_t)(stats + (uint32_t)(t * kWaves * 16 + col) * 8);
+    const auto* st = (const __attribute__((address_space(3))) float*)(stats + (t * kWaves * 16 + col) * 8);
 #pragma unroll
     for (int y = 0; y < kWaves; ++y) {
       m[y] = st[32 * y];
@@ -452,21 +455,23 @@ __device__ inline void attend(const SharedParams& p, const SharedCache& c, int s
 #pragma unroll
     for (int y = 0; y < kWaves; ++y) l = __builtin_fmaf(st[32 * y + 1], __builtin_amdgcn_exp2f(m[y] - top), l);
     const float mine = __builtin_amdgcn_exp2f(ref[t] - top);
-    const uint32_t area = lds0 + (uint32_t)((t & 1) * kWaves * 8192);
+    const lds_at area = lds0 + (t & 1) * kWaves * 8192;
 #pragma unroll
     for (int x = 0; x < 8; ++x) {
       floatx4 v = o[t][x] * mine;
-      lds_write16(area + (uint32_t)((x * kWaves + wave) * 1024 + 16 * lane), __builtin_bit_cast(uintx4, v));
+      lds_write16(area + wave * 1024 + 16 * lane + x * kWaves * 1024, __builtin_bit_cast(uintx4, v));
     }
     __syncthreads();
-    floatx4 v = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-    for (int y = 0; y < kWaves; ++y) v += __builtin_bit_cast(floatx4, lds_read16(area + (uint32_t)((wave * kWaves + y) * 1024 + 16 * lane)));
     const int row = 16 * t + col;
-    if (row < rows) {
-      *(floatx4*)(p.parts + (slot0 + row) * TKV_D + 16 * wave + 4 * kb) = v;
-      if (wave == 0 && kb == 0) *(float2*)(p.ml + (slot0 + row) * 2) = make_float2(top, l);
+#pragma unroll
+    for (int z = 0; z < 8 / kWaves; ++z) {
+      const int x = wave * (8 / kWaves) + z;
+      floatx4 v = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int y = 0; y < kWaves; ++y) v += __builtin_bit_cast(floatx4, lds_read16(area + x * kWaves * 1024 + 16 * lane + y * 1024));
+      if (row < rows) *(floatx4*)(p.parts + (slot0 + row) * TKV_D + 16 * x + 4 * kb) = v;
     }
+    if (row < rows && wave == 0 && kb == 0) *(float2*)(p.ml + (slot0 + row) * 2) = make_float2(top, l);
   }
 }
 
