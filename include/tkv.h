@@ -227,7 +227,7 @@ int32_t tkv_quant_attn_decode_shared_sizes(const tkv_quant_desc* prefix_desc, co
  * tkv_quant_attn_decode over a cache that held prefix and own tokens, quantized as they are here: the prefix's
  * newest tokens stay fp16 as its own descriptor says.
  * prefix_desc and desc: same heads, bits and group_size; residual, capacity and batch may differ.  Either may hold empty
- * sequences; a sequence without any token yields zeros.  q (a multiple of 4 bytes), out: fp16 [B][Hq][128].  sm_scale > 0.
+ * sequences; a sequence without any token yields zeros.  q, out: fp16 [B][Hq][128], at multiples of 4 bytes.  sm_scale > 0.
  * All six settings of bits and group_size are evaluated alike: code*s + z rounded to fp16, products of fp16 numbers with float32
  * sums, softmax statistics in float32, its weights rounded to fp16.  Cached values of magnitude up to 30000 are safe (a
  * dequantized value beyond 65504 is infinite).  The result is the same bit for bit from call to call.

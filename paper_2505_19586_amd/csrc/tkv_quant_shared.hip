@@ -123,7 +123,7 @@ constexpr int lds_bytes() {
 
 // One segment's rows (16 NQ of them) over one chunk of its tokens.
 template <int BITS, int GS, int NQ, int MAXQ>
-__device__ inline void attend(const SharedParams& p, const SharedCache& c, int seq, int n, int h, int chunk, int chunks,
+__device__ __attribute__((always_inline)) inline void attend(const SharedParams& p, const SharedCache& c, int seq, int n, int h, int chunk, int chunks,
                               const uint8_t* order, int row0, int rows, int64_t slot0) {
   constexpr int G = 32 * GS, CB = code_bytes<BITS>(), SB = slot_bytes<BITS>();
   extern __shared__ __attribute__((aligned(1024))) char lds[];
@@ -143,35 +143,44 @@ __device__ inline void attend(const SharedParams& p, const SharedCache& c, int s
   const int64_t head = (int64_t)seq * p.hkv + h;
   const char* kc = c.k_codes + head * c.capacity * (16 * BITS);
   const char* vc = c.v_codes + head * c.capacity * (16 * BITS);
-  // a lane's sixteen bytes of a block's scalers and zero-points: k_scale, k_zero, v_scale, v_zero, 256 bytes each (values in groups
-  // of 64: 128, read twice)
-  const char* meta;
-  uint32_t meta_step;   // from block to block; keys in groups of 64: from pair to pair
+  // The block that is sent for next: its keys' and values' codes, and a lane's sixteen bytes of its scalers and zero-points: k_scale,
+  // k_zero, v_scale, v_zero, 256 bytes each (values in groups of 64: 128, read twice).
+  const char* next_k = kc + (int64_t)b0 * (512 * BITS);
+  const char* next_v = vc + (int64_t)b0 * (512 * BITS);
+  const char* next_meta;
+  uint32_t step_even, step_odd;  // from an even block to the next, from an odd one (keys in groups of 64: every other time)
   {
     const int64_t per_head = (int64_t)c.capacity * (256 / G);  // bytes: tokens / G groups of 128 fp16; as many for values
     if (kb < 2) {
-      meta = (kb ? c.k_zero : c.k_scale) + head * per_head + 16 * col;
-      meta_step = 256;
+      next_meta = (kb ? c.k_zero : c.k_scale) + head * per_head + 16 * col + (int64_t)(b0 / GS) * 256;
+      step_even = GS == 2 ? 0u : 256u;
+      step_odd = 256u;
     } else {
-      meta = (kb == 3 ? c.v_zero : c.v_scale) + head * per_head + 16 * (GS == 2 ? col % 8 : col);
-      meta_step = 256 / GS;
+      next_meta = (kb == 3 ? c.v_zero : c.v_scale) + head * per_head + 16 * (GS == 2 ? col % 8 : col) + (int64_t)b0 * (256 / GS);
+      step_even = step_odd = 256u / GS;
     }
   }
-  auto stage = [&](int slot, int j) {
+  const uint32_t lane_at = BITS == 1 ? 16u * (uint32_t)(lane % 32) : 16u * (uint32_t)lane;
+  auto stage = [&](int slot) {
     const uint32_t to = (uint32_t)(uintptr_t)(ring + slot * SB);
-    const uint32_t mine = BITS == 1 ? 16u * (uint32_t)(lane % 32) : 16u * (uint32_t)lane;
-    const int64_t at = (int64_t)j * (512 * BITS);
 #pragma unroll
-    for (int y = 0; y < CB / 1024; ++y) to_lds(kc + at + 1024 * y, mine, to + 1024 * y);
+    for (int y = 0; y < CB / 1024; ++y) to_lds(next_k + 1024 * y, lane_at, to + 1024 * y);
 #pragma unroll
-    for (int y = 0; y < CB / 1024; ++y) to_lds(vc + at + 1024 * y, mine, to + CB + 1024 * y);
-    to_lds(meta + (uint64_t)(uint32_t)(GS == 2 && kb < 2 ? j / 2 : j) * meta_step, to + 2 * CB);
+    for (int y = 0; y < CB / 1024; ++y) to_lds(next_v + 1024 * y, lane_at, to + CB + 1024 * y);
+    to_lds(next_meta, to + 2 * CB);
+  };
+  auto advance = [&](int j, int end) {  // from block j, where there is one behind it (otherwise it is sent for again)
+    const uint32_t on = j + 1 < end ? 1u : 0u;
+    next_k += on * (512 * BITS);
+    next_v += on * (512 * BITS);
+    next_meta += on * (GS == 2 && j % 2 == 0 ? step_even : step_odd);
   };
   constexpr int kLoads = 2 * (CB / 1024) + 1;
   const int c1 = min(b1, coded);  // quantized blocks [b0, c1), then pieces of the ring [max(b0, coded), b1)
   if (b0 < c1) {
-    stage(0, b0);
-    stage(1, min(b0 + 1, c1 - 1));
+    stage(0);
+    advance(b0, c1);
+    stage(1);
   }
 
   // the rows' queries in operand order, shared by all waves: wave w lays out tiles w, w + 8, ...
@@ -187,6 +196,9 @@ __device__ inline void attend(const SharedParams& p, const SharedCache& c, int s
   }
   __syncthreads();
 
+  // (Two waves of a SIMD in step wait for the matrix cores and for the vector unit at the same time; with one of them always first they
+  // fall out of step: 65.9 -> 64.6 us for 131072 tokens under 16 sequences, 138 -> 134 for 32770 under 64 at 4 bits.)
+  if (wave >= kWaves / 2) __builtin_amdgcn_s_setprio(2);
   floatx4 o[NQ][8];
   float ref[NQ], sum[NQ];
 #pragma unroll
@@ -302,13 +314,10 @@ __device__ inline void attend(const SharedParams& p, const SharedCache& c, int s
       term_at = terms;
     }
     // (the next block but one goes where the previous block was, whose reads are done)
-    stage(slot == 0 ? 2 : slot - 1, min(j + 2, c1 - 1));
+    advance(j + 1, c1);
+    stage(slot == 0 ? 2 : slot - 1);
     const lds_at at = ring + slot * SB;
     slot = slot == kSlots - 1 ? 0 : slot + 1;
-    float base[NQ];
-#pragma unroll
-    for (int t = 0; t < NQ; ++t) base[t] = __uint_as_float(lds_word(term_at + 4 * col + 64 * t));
-    if (GS == 1 || j % 2 == 1) term_at += NQ * 64;
     floatx4 s[2][NQ];
 #pragma unroll
     for (int t = 0; t < NQ; ++t) s[0][t] = s[1][t] = (floatx4){0.f, 0.f, 0.f, 0.f};
@@ -342,6 +351,10 @@ __device__ inline void attend(const SharedParams& p, const SharedCache& c, int s
     keys(std::integral_constant<int, 0>{});
     keys(std::integral_constant<int, 1>{});
     keys(std::integral_constant<int, 2>{});
+    float base[NQ];
+#pragma unroll
+    for (int t = 0; t < NQ; ++t) base[t] = __uint_as_float(lds_word(term_at + 4 * col + 64 * t));
+    if (GS == 1 || j % 2 == 1) term_at += NQ * 64;
     keys(std::integral_constant<int, 3>{});
     constexpr int U = 128 / G;
     uint32_t vw[8];
@@ -476,7 +489,7 @@ __device__ inline void attend(const SharedParams& p, const SharedCache& c, int s
 }
 
 template <int BITS, int GS, int NQ>
-__global__ __launch_bounds__(64 * kWaves, 2) void shared_attn_kernel(SharedParams p) {
+__global__ __launch_bounds__(64 * kWaves, NQ == 1 ? 4 : 2) void shared_attn_kernel(SharedParams p) {
   const int lane = threadIdx.x % 64;
   const int h = blockIdx.x % p.hkv, it = blockIdx.x / p.hkv;
   const bool own = it >= p.prefix_items;
@@ -497,48 +510,76 @@ __global__ __launch_bounds__(64 * kWaves, 2) void shared_attn_kernel(SharedParam
   }
 }
 
-// Joins a query head's partial results, those of its prefix's chunks and of its own: a workgroup per head, every wave a quarter of
-// the parts, a lane two channels.
+// Joins a query head's partial results, those of its prefix's chunks and of its own, a lane two channels.  ONE: a wave per head;
+// otherwise a workgroup, every wave a quarter of the parts.  (64 sequences of 64 heads, about 10 parts each: 4.9 us with a wave,
+// 11.0 with a workgroup; whole calls of 16 sequences of 32 heads, 29 parts: 67.7, 65.9; 8 of 32, about 40 parts: 27.5, 24.9.)
+template <bool ONE>
 __global__ __launch_bounds__(256) void shared_merge_kernel(SharedParams p) {
-  __shared__ float acc_s[4][TKV_D], l_s[4];
-  const int lane = threadIdx.x % 64, wave = threadIdx.x / 64;
-  const int b = blockIdx.x / p.hq, head = blockIdx.x % p.hq, h = head / p.group, g = head % p.group;
-  const int pf = p.prefix_of[b], rows = pf == 255 ? 0 : p.p_count[pf] * p.group;
-  const int n_p = pf == 255 ? 0 : p.p_chunks[pf], n_o = p.chunks[b];
-  const int64_t base_p = pf == 255 ? 0 : p.p_slot[pf] + (int64_t)h * n_p * rows + p.rank[b] * p.group + g;
-  const int64_t base_o = p.slot[b] + (int64_t)h * n_o * p.group + g;
-  auto slot_of = [&](int i) { return i < n_p ? base_p + (int64_t)i * rows : base_o + (int64_t)(i - n_p) * p.group; };
-  const int n = n_p + n_o;
-  float m = kNone;
-  for (int i = threadIdx.x % 64; i < n; i += 64) m = fmaxf(m, p.ml[slot_of(i) * 2]);
-  m = tkv::over_wave(m, tkv::MaxOf{});
+  __shared__ float acc_s[4][TKV_D], l_s[4], m_s[4];
+  const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
+  const int row = ONE ? 4 * blockIdx.x + wave : blockIdx.x, first = ONE ? 0 : wave;
+  constexpr int kStep = ONE ? 1 : 4;
+  if (row >= p.batch * p.hq) return;
+  const int b = row / p.hq, head = row % p.hq, h = head / p.group, g = head % p.group;
+  const int pf = p.prefix_of[b], at_p = min(pf, TKV_MAX_BATCH - 1);
+  const bool none = pf == 255;
+  const int rows = none ? 0 : p.p_count[at_p] * p.group, n_p = none ? 0 : p.p_chunks[at_p], n = n_p + p.chunks[b];
+  const int64_t base_p = p.p_slot[at_p] + (int64_t)h * n_p * rows + p.rank[b] * p.group + g;
+  const int64_t base_o = p.slot[b] + (int64_t)h * p.chunks[b] * p.group + g;
+  float m = kNone, l = 0.f;
   float2 acc = make_float2(0.f, 0.f);
-  float l = 0.f;
-#pragma unroll 8
-  for (int i = wave; i < n; i += 4) {
-    const int64_t s = slot_of(i);
-    const float2 st = *(const float2*)(p.ml + s * 2), v = *(const float2*)(p.parts + s * TKV_D + 2 * lane);
-    const float w = __builtin_amdgcn_exp2f(st.x - m);
-    l = __builtin_fmaf(st.y, w, l);
-    acc.x = __builtin_fmaf(v.x, w, acc.x);
-    acc.y = __builtin_fmaf(v.y, w, acc.y);
+  // (requests of eight parts at a time, absent ones those of the first with a weight of zero)
+  for (int i0 = first; i0 < n; i0 += 8 * kStep) {
+    float2 st[8], v[8];
+#pragma unroll
+    for (int y = 0; y < 8; ++y) {
+      const int i = i0 + kStep * y < n ? i0 + kStep * y : i0;
+      const int64_t s = i < n_p ? base_p + (int64_t)i * rows : base_o + (int64_t)(i - n_p) * p.group;
+      st[y] = *(const float2*)(p.ml + s * 2);
+      v[y] = *(const float2*)(p.parts + s * TKV_D + 2 * lane);
+    }
+    float top = m;
+#pragma unroll
+    for (int y = 0; y < 8; ++y) top = fmaxf(top, st[y].x);
+    const float shrink = __builtin_amdgcn_exp2f(m - top);
+    m = top;
+    l *= shrink;
+    acc.x *= shrink;
+    acc.y *= shrink;
+#pragma unroll
+    for (int y = 0; y < 8; ++y) {
+      const float w = i0 + kStep * y < n ? __builtin_amdgcn_exp2f(st[y].x - m) : 0.f;
+      l = __builtin_fmaf(st[y].y, w, l);
+      acc.x = __builtin_fmaf(v[y].x, w, acc.x);
+      acc.y = __builtin_fmaf(v[y].y, w, acc.y);
+    }
+  }
+  if constexpr (ONE) {
+    const float inv = l == 0.f ? 0.f : 1.f / l;
+    *(__half2*)(p.out + (int64_t)row * TKV_D + 2 * lane) = __floats2half2_rn(acc.x * inv, acc.y * inv);
+    return;
   }
   *(float2*)(acc_s[wave] + 2 * lane) = acc;
-  if (lane == 0) l_s[wave] = l;
+  if (lane == 0) l_s[wave] = l, m_s[wave] = m;
   __syncthreads();
-  if (threadIdx.x < TKV_D) {
-    const int c = threadIdx.x;
-    const float total = l_s[0] + l_s[1] + l_s[2] + l_s[3];
-    const float v = acc_s[0][c] + acc_s[1][c] + acc_s[2][c] + acc_s[3][c];
-    p.out[((int64_t)b * p.hq + head) * TKV_D + c] = __float2half_rn(total == 0.f ? 0.f : v / total);
+  if (threadIdx.x >= TKV_D) return;
+  const int c = threadIdx.x;
+  const float top = fmaxf(fmaxf(m_s[0], m_s[1]), fmaxf(m_s[2], m_s[3]));
+  float total = 0.f, v = 0.f;
+#pragma unroll
+  for (int w = 0; w < 4; ++w) {
+    const float f = __builtin_amdgcn_exp2f(m_s[w] - top);
+    total = __builtin_fmaf(l_s[w], f, total);
+    v = __builtin_fmaf(acc_s[w][c], f, v);
   }
+  p.out[(int64_t)row * TKV_D + c] = __float2half_rn(total == 0.f ? 0.f : v / total);
 }
 
-// Cost of a block of 32 tokens for a row group of 16 NQ, in units of a vector instruction: unpacking, then logits and weights of
-// every tile.
-constexpr int block_cost(int nq) { return 200 + 66 * nq; }
-constexpr int kFixedCost = 6000;  // ... of a workgroup beside its blocks (a first round trip, the join of its waves)
-constexpr int kWorkgroups = 256;  // one per compute unit (a workgroup takes most of its LDS)
+// What a workgroup takes, in units of 0.8 ns: a block of 32 tokens for a row group of 16 NQ, and its fixed part (a first round
+// trip, the join of its waves); measured at 2 bits.
+constexpr double block_cost(int nq) { return nq == 1 ? 200 : nq == 2 ? 300 : 464; }
+constexpr double fixed_cost(int nq) { return nq == 1 ? 6000 : nq == 2 ? 8000 : 10000; }
+constexpr int kWorkgroups = 256;  // workgroups at a time: one per compute unit (it takes most of the LDS)
 
 int tiles_of(int rows) { return rows <= 16 ? 1 : rows <= 32 ? 2 : 4; }
 
@@ -603,7 +644,7 @@ extern "C" int32_t tkv_quant_attn_decode_shared(const tkv_quant_desc* pd, const 
   const int32_t st = check_pair(pd, d);
   if (st != TKV_OK) return st;
   if (!cache_ok(prefix) || !cache_ok(cache) || !q || !out || !workspace) return TKV_E_INVAL;
-  if (((uintptr_t)q & 3) != 0 || ((uintptr_t)out & 1) != 0 || ((uintptr_t)workspace & 15) != 0) return TKV_E_INVAL;
+  if (((uintptr_t)q & 3) != 0 || ((uintptr_t)out & 3) != 0 || ((uintptr_t)workspace & 15) != 0) return TKV_E_INVAL;
   if (!(sm_scale > 0.f) || !(sm_scale <= 3.402823466e38f)) return TKV_E_INVAL;
   for (int i = 0; i < pd->batch; ++i)
     if (prefix->seq_len_host[i] < 0 || prefix->seq_len_host[i] > pd->capacity) return TKV_E_INVAL;
@@ -639,56 +680,80 @@ extern "C" int32_t tkv_quant_attn_decode_shared(const tkv_quant_desc* pd, const 
     p.p_count[i] = (uint8_t)(at - p.p_begin[i]);
     if (p.p_count[i] > most) most = p.p_count[i];
   }
-  int64_t own_blocks[TKV_MAX_BATCH], prefix_blocks[TKV_MAX_BATCH];
+  int64_t own_blocks[TKV_MAX_BATCH], prefix_blocks[TKV_MAX_BATCH], longest = 0;
   const int tiles = tiles_of(most * p.group);
   auto groups_of = [&](int i) { return (p.p_count[i] * p.group + 16 * tiles - 1) / (16 * tiles); };
-  double cost = 0;
+  double all = 0;
   for (int b = 0; b < d->batch; ++b) {
     if (prefix_of_host && prefix_of_host[b] < 0) p.prefix_of[b] = 255, p.rank[b] = 0;
     p.len[b] = cache->seq_len_host[b];
     own_blocks[b] = blocks_of(d, p.len[b]);
-    cost += (double)own_blocks[b] * block_cost(1);
+    all += (double)own_blocks[b] * block_cost(1);
+    if (own_blocks[b] > longest) longest = own_blocks[b];
   }
   for (int i = 0; i < pd->batch; ++i) {
     prefix_blocks[i] = p.p_count[i] ? blocks_of(pd, p.p_len[i]) : 0;
-    cost += (double)prefix_blocks[i] * groups_of(i) * block_cost(tiles);
+    all += (double)prefix_blocks[i] * groups_of(i) * block_cost(tiles);
+    if (prefix_blocks[i] > longest) longest = prefix_blocks[i];
   }
-  cost *= p.hkv;
+  all *= p.hkv;
 
-  // Chunks of at most `per` each, no smaller than a block per wave, such that the workgroups fit one round of the compute units;
-  // chunks of less than `per` count as that share of one (they come last and fill what is left).
-  int64_t items = 0, slots = 0;
-  double per = cost / kWorkgroups;
-  for (int turn = 0;; ++turn, per *= 1.04) {
-    double used = 0;
-    auto chunks_of = [&](int64_t blocks, int c, int copies) {
-      if (blocks == 0) return 0;
-      const double all = (double)blocks * c;
-      int64_t n = per > 1 ? (int64_t)(all / per) : blocks;
-      if ((double)n * per < all) ++n;
-      const int64_t fill = (blocks + kWaves - 1) / kWaves;
-      n = n < fill ? n : fill;
-      const double share = (all / n + kFixedCost) / (per + kFixedCost);
-      used += (double)n * copies * p.hkv * (share < 0.5 ? share : 1.0);
-      return (int)n;
-    };
-    items = slots = 0;
+  // Chunks of at most `per` each, no smaller than a block per wave.  Of a dozen sizes from an even share of everything on, the one with the
+  // shortest time: rounds of the prefixes' workgroups, which come first, or everything shared out evenly, the last own
+  // ones behind it.
+  auto chunks_of = [](int64_t blocks, double cost, double per) {
+    const double whole = (double)blocks * cost;
+    int64_t n = (int64_t)(whole / per);
+    if ((double)n * per < whole) ++n;
+    const int64_t fill = (blocks + kWaves - 1) / kWaves;
+    return (int32_t)(n < fill ? n : fill);
+  };
+  const double even = all / kWorkgroups > 1 ? all / kWorkgroups : 1;
+  double best = even, least = 0;
+  for (double per = even; per < 4 * even && per < 1.2 * (double)longest * block_cost(tiles) + 1; per *= 1.12) {
+    double n_prefix = 0, n_own = 0, long_prefix = 0, long_own = 0, sum = 0;
     for (int i = 0; i < pd->batch; ++i) {
-      p.p_chunks[i] = chunks_of(prefix_blocks[i], block_cost(tiles), groups_of(i));
-      p.p_first[i] = (int32_t)items;
-      p.p_slot[i] = (int32_t)slots;
-      items += (int64_t)p.p_chunks[i] * groups_of(i);
-      slots += (int64_t)p.p_chunks[i] * p.p_count[i] * p.group * p.hkv;
+      const int n = chunks_of(prefix_blocks[i], block_cost(tiles), per), copies = groups_of(i) * p.hkv;
+      if (n == 0) continue;
+      const double each = (double)prefix_blocks[i] * block_cost(tiles) / n + fixed_cost(tiles);
+      n_prefix += (double)n * copies;
+      sum += each * n * copies;
+      if (each > long_prefix) long_prefix = each;
     }
-    p.prefix_items = (int32_t)items;
     for (int b = 0; b < d->batch; ++b) {
-      p.chunks[b] = chunks_of(own_blocks[b], block_cost(1), 1);
-      p.first[b] = (int32_t)items;
-      p.slot[b] = (int32_t)slots;
-      items += p.chunks[b];
-      slots += (int64_t)p.chunks[b] * p.group * p.hkv;
+      const int n = chunks_of(own_blocks[b], block_cost(1), per);
+      if (n == 0) continue;
+      const double each = (double)own_blocks[b] * block_cost(1) / n + fixed_cost(1);
+      n_own += (double)n * p.hkv;
+      sum += each * n * p.hkv;
+      if (each > long_own) long_own = each;
     }
-    if (used <= kWorkgroups || turn == 40) break;
+    double time = (double)(int64_t)((n_prefix + kWorkgroups - 1) / kWorkgroups) * long_prefix;
+    const double shared_out = sum / kWorkgroups + (n_prefix + n_own > kWorkgroups ? long_own / 2 : 0);
+    if (shared_out > time) time = shared_out;
+    if (long_own > time) time = long_own;
+    if (least == 0 || time < least) least = time, best = per;
+  }
+  int64_t items = 0, slots = 0;
+  for (int i = 0; i < pd->batch; ++i) {
+    p.p_chunks[i] = chunks_of(prefix_blocks[i], block_cost(tiles), best);
+    p.p_first[i] = (int32_t)items;
+    p.p_slot[i] = (int32_t)slots;
+    items += (int64_t)p.p_chunks[i] * groups_of(i);
+    slots += (int64_t)p.p_chunks[i] * p.p_count[i] * p.group * p.hkv;
+  }
+  p.prefix_items = (int32_t)items;
+  for (int b = 0; b < d->batch; ++b) {
+    p.chunks[b] = chunks_of(own_blocks[b], block_cost(1), best);
+    p.first[b] = (int32_t)items;
+    p.slot[b] = (int32_t)slots;
+    items += p.chunks[b];
+    slots += (int64_t)p.chunks[b] * p.group * p.hkv;
+  }
+  int most_parts = 0;
+  for (int b = 0; b < d->batch; ++b) {
+    const int n = p.chunks[b] + (p.prefix_of[b] == 255 ? 0 : p.p_chunks[p.prefix_of[b]]);
+    if (n > most_parts) most_parts = n;
   }
   if (slots > slots_max) return TKV_E_WORKSPACE;  // (cannot be)
 
@@ -706,6 +771,8 @@ extern "C" int32_t tkv_quant_attn_decode_shared(const tkv_quant_desc* pd, const 
     }
     if (r != TKV_OK) return r;
   }
-  TKV_LAUNCH(shared_merge_kernel, dim3((uint32_t)(p.batch * p.hq)), 256, 0, s, p);
+  const uint32_t heads = (uint32_t)(p.batch * p.hq);
+  if (most_parts <= 16) TKV_LAUNCH(shared_merge_kernel<true>, dim3((heads + 3) / 4), 256, 0, s, p);
+  else TKV_LAUNCH(shared_merge_kernel<false>, dim3(heads), 256, 0, s, p);
   return TKV_OK;
 }

@@ -43,7 +43,7 @@ def _call(L, prefix=None, own=None, prefix_lens=(100, 4096), lens=(5, 0, 7), of=
     (dict(own=dict(head_dim=64)), -2), (dict(prefix_lens=(100, 4097)), -1), (dict(lens=(5, -1, 0)), -1),
     (dict(of=(0, 2, 0)), -1), (dict(of=(0, -2, 0)), -1), (dict(sm=0.0), -1), (dict(sm=float("nan")), -1), (dict(sm=float("inf")), -1),
     (dict(ws=1000), -4), (dict(ptr=dict(ws=0)), -1), (dict(ptr=dict(ws=A + 4)), -1), (dict(ptr=dict(q=A + 2)), -1),
-    (dict(ptr=dict(q=0)), -1), (dict(ptr=dict(out=0)), -1), (dict(ptr=dict(out=A + 1)), -1), (dict(cache=dict(k_codes=0)), -1),
+    (dict(ptr=dict(q=0)), -1), (dict(ptr=dict(out=0)), -1), (dict(ptr=dict(out=A + 2)), -1), (dict(cache=dict(k_codes=0)), -1),
     (dict(cache=dict(v_zero=A + 2)), -1), (dict(cache=dict(seq_len_host=None)), -1),
 ])
 def test_refusals(L, kw, status):
