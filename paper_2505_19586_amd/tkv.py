@@ -4,6 +4,8 @@ is no CPU or PyTorch fallback - a missing library or GPU raises."""
 from __future__ import annotations
 
 import ctypes as C
+import itertools
+import operator
 import os
 
 import numpy as np
@@ -62,14 +64,15 @@ class RopeDesc(C.Structure):
     _fields_ = [("struct_size", C.c_uint32), ("n_q_heads", C.c_int32), ("n_kv_heads", C.c_int32),
                 ("head_dim", C.c_int32), ("in_dtype", C.c_int32), ("out_dtype", C.c_int32), ("norm", C.c_int32),
                 ("eps", C.c_float), ("rotary_dim", C.c_int32), ("interleaved", C.c_int32),
-                ("q_stride", C.c_int64 * 2), ("k_stride", C.c_int64 * 2), ("v_stride", C.c_int64 * 2)]
+                # (strides of tokens and heads; single fields, as an array each costs a third of a microsecond to fill)
+                ("q_stride", C.c_int64), ("q_stride_head", C.c_int64), ("k_stride", C.c_int64),
+                ("k_stride_head", C.c_int64), ("v_stride", C.c_int64), ("v_stride_head", C.c_int64)]
 
 
 class PromptDesc(C.Structure):
     _fields_ = [("struct_size", C.c_uint32), ("n_q_heads", C.c_int32), ("n_kv_heads", C.c_int32),
                 ("head_dim", C.c_int32), ("dtype", C.c_int32), ("causal", C.c_int32), ("batch", C.c_int32),
-                ("reserved", C.c_int32), ("q_stride", C.c_int64 * 2), ("k_stride", C.c_int64 * 2),
-                ("v_stride", C.c_int64 * 2), ("o_stride", C.c_int64 * 2)]
+                ("reserved", C.c_int32), ("strides", C.c_int64 * 8)]  # of tokens and heads: q, k, v, out
 
 
 def lib() -> C.CDLL:
@@ -588,43 +591,42 @@ def qk_norm_rope(q: torch.Tensor, k: torch.Tensor, positions: torch.Tensor | Non
     """tkv_qk_norm_rope: q [T, Hq, 128], k, v [T, Hkv, 128] (fp16 or bf16, views of one fused projection
     allowed), positions int32 [T], inv_freq float32 [R/2] (None: no rotation) -> contiguous (q_out, k_out, v_out or
     None) in out_dtype (default: the inputs')."""
-    assert q.is_cuda and q.dim() == 3 and k.dim() == 3 and k.shape[0] == q.shape[0] and k.shape[2] == q.shape[2]
+    t, hq, ch = q.shape
+    t2, hkv, ch2 = k.shape
+    dt, dev = q.dtype, q.device
+    assert q.is_cuda and t2 == t and ch2 == ch and k.dtype == dt and k.device == dev
     _on_current(q, stream)
-    t, dt = q.shape[0], q.dtype
-    for x in (k, v, q_weight, k_weight):
-        assert x is None or (x.dtype == dt and x.device == q.device)
-    for x in (q, k, v):
-        assert x is None or x.stride(2) == 1
-    assert v is None or v.shape == k.shape
+    sq, sk, sv = q.stride(), k.stride(), (0, 0, 1)
+    if v is not None:
+        assert v.shape == k.shape and v.dtype == dt and v.device == dev
+        sv = v.stride()
+    assert sq[2] == 1 and sk[2] == 1 and sv[2] == 1
     rot = 0
     if inv_freq is not None:
-        assert inv_freq.dtype == torch.float32 and inv_freq.device == q.device and inv_freq.dim() == 1 and inv_freq.is_contiguous()
-        assert positions is not None and positions.dtype == torch.int32 and positions.device == q.device
-        assert tuple(positions.shape) == (t,) and positions.is_contiguous()
+        assert inv_freq.dtype == torch.float32 and inv_freq.dim() == 1 and inv_freq.is_contiguous() and inv_freq.device == dev
+        assert positions is not None and positions.dtype == torch.int32 and positions.device == dev
+        assert positions.shape == (t,) and positions.is_contiguous()
         rot = 2 * inv_freq.shape[0]
     for w in (q_weight, k_weight):
-        assert w is None or (tuple(w.shape) == (q.shape[2],) and w.is_contiguous())
+        assert w is None or (w.shape == (ch,) and w.is_contiguous() and w.dtype == dt and w.device == dev)
     if out_dtype is None:
         out_dtype = next((x.dtype for x in (q_out, k_out, v_out) if x is not None), dt)
-    outs = []
     for x, o in ((q, q_out), (k, k_out), (v, v_out)):
-        if x is None:
-            assert o is None
-        elif o is None:
-            o = torch.empty(x.shape, dtype=out_dtype, device=q.device)
-        else:
-            assert o.dtype == out_dtype and o.shape == x.shape and o.is_contiguous() and o.device == q.device
-        outs.append(o)
-
-    def strides(x):  # (an axis of one element: torch leaves its stride to chance)
-        return (C.c_int64 * 2)() if x is None else (C.c_int64 * 2)(x.stride(0) if t > 1 else 0, x.stride(1) if x.shape[1] > 1 else 0)
-
-    desc = RopeDesc(C.sizeof(RopeDesc), q.shape[1], k.shape[1], q.shape[2], _DTYPES.get(dt, -1), _DTYPES.get(out_dtype, -1),
-                    int(norm), float(eps), rot, int(interleaved), strides(q), strides(k), strides(v))
+        assert o is None or (x is not None and o.dtype == out_dtype and o.shape == x.shape and o.is_contiguous() and o.device == dev)
+    if q_out is None:
+        q_out = torch.empty((t, hq, ch), dtype=out_dtype, device=dev)
+    if k_out is None:
+        k_out = torch.empty((t, hkv, ch), dtype=out_dtype, device=dev)
+    if v_out is None and v is not None:
+        v_out = torch.empty((t, hkv, ch), dtype=out_dtype, device=dev)
+    # (an axis of one element: torch leaves its stride to chance)
+    by_t, by_q, by_k = t > 1, hq > 1, hkv > 1
+    desc = RopeDesc(C.sizeof(RopeDesc), hq, hkv, ch, _DTYPES.get(dt, -1), _DTYPES.get(out_dtype, -1), norm, eps, rot, interleaved,
+                    by_t * sq[0], by_q * sq[1], by_t * sk[0], by_k * sk[1], by_t * sv[0], by_k * sv[1])
     _check(lib().tkv_qk_norm_rope(C.byref(desc), t, q.data_ptr(), k.data_ptr(), _ptr(v), _ptr(positions) if rot else 0,
-                                  _ptr(inv_freq) if rot else 0, _ptr(q_weight), _ptr(k_weight), outs[0].data_ptr(), outs[1].data_ptr(),
-                                  _ptr(outs[2]), _stream(stream)), "tkv_qk_norm_rope")
-    return tuple(outs)
+                                  _ptr(inv_freq) if rot else 0, _ptr(q_weight), _ptr(k_weight), q_out.data_ptr(), k_out.data_ptr(),
+                                  _ptr(v_out), _stream(stream)), "tkv_qk_norm_rope")
+    return q_out, k_out, v_out
 
 
 class PromptAttention:
@@ -640,6 +642,7 @@ class PromptAttention:
         self.workspace = torch.empty(self.workspace_bytes, dtype=torch.uint8, device=dev)
         self.dtype = dtype
         self.device = dev
+        self._q_row, self._k_row = (n_q_heads, head_dim), (n_kv_heads, head_dim)
 
     def attend(self, q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, sm_scale: float, q_lens, k_lens=None, *,
                q_starts=None, k_starts=None, out: torch.Tensor | None = None, lse: bool | torch.Tensor = False, stream=None):
@@ -647,41 +650,45 @@ class PromptAttention:
         every sequence, one after the other unless q_starts / k_starts say where each begins.  Returns out
         [Tq, Hq, 128], or (out, lse [Tq, Hq]) where lse is True or a float32 tensor.  Rows of no sequence are left as they
         were (a new out has zeros there)."""
-        d = self.desc
-        assert q.is_cuda and q.dim() == 3 and k.dim() == 3 and k.shape == v.shape
+        d, n = self.desc, self.desc.batch
+        rows_q, rows_k = q.shape[0], k.shape[0]
+        assert q.is_cuda and k.shape == v.shape and q.shape[1:] == self._q_row and k.shape[1:] == self._k_row
         assert q.dtype == k.dtype == v.dtype == self.dtype and q.device == k.device == v.device == self.workspace.device
-        assert tuple(q.shape[1:]) == (d.n_q_heads, d.head_dim) and tuple(k.shape[1:]) == (d.n_kv_heads, d.head_dim)
-        assert q.stride(2) == 1 and k.stride(2) == 1 and v.stride(2) == 1
         _on_current(q, stream)
-        lens = np.empty((4, d.batch), dtype=np.int32)   # q_start, q_len, k_start, k_len
-        lens[1] = q_lens
-        lens[3] = q_lens if k_lens is None else k_lens
-        rows = (q.shape[0], 0, k.shape[0])
-        packed = q_starts is None
-        for i, given in ((0, q_starts), (2, k_starts)):
-            if given is None:
-                lens[i, 0] = 0
-                np.cumsum(lens[i + 1, :-1], out=lens[i, 1:])
-            else:
-                lens[i] = given
-            assert lens[i].min() >= 0 and lens[i + 1].min() >= 0
-            assert int((lens[i].astype(np.int64) + lens[i + 1]).max()) <= rows[i], "a sequence reaches past the tensor's rows"
+
+        def ints(x, what):
+            x = [int(i) for i in x]
+            assert len(x) == n and min(x) >= 0, f"{what}: {n} numbers, none below 0"
+            return x
+
+        def begin(starts, lens, rows, what):  # (one after the other unless given)
+            starts = [0, *itertools.accumulate(lens[:-1])] if starts is None else ints(starts, what)
+            assert max(map(operator.add, starts, lens)) <= rows, "a sequence reaches past the tensor's rows"
+            return starts
+
+        q_lens = ints(q_lens, "q_lens")
+        k_lens = q_lens if k_lens is None else ints(k_lens, "k_lens")
+        whole = q_starts is None and sum(q_lens) == rows_q  # every row is some sequence's
+        lens = [(C.c_int32 * n)(*x) for x in (begin(q_starts, q_lens, rows_q, "q_starts"), q_lens,
+                                              begin(k_starts, k_lens, rows_k, "k_starts"), k_lens)]
         if out is None:
-            out = (torch.empty if packed and int(lens[1].sum()) == q.shape[0] else torch.zeros)(q.shape, dtype=q.dtype, device=q.device)
+            out = (torch.empty if whole else torch.zeros)(q.shape, dtype=q.dtype, device=q.device)
         else:
-            assert out.dtype == q.dtype and out.shape == q.shape and out.device == q.device and out.stride(2) == 1
+            assert out.dtype == q.dtype and out.shape == q.shape and out.device == q.device
         if lse is True:
-            lse = torch.full(q.shape[:2], -float("inf"), dtype=torch.float32, device=q.device) if not packed or int(lens[1].sum()) != q.shape[0] \
-                else torch.empty(q.shape[:2], dtype=torch.float32, device=q.device)
+            lse = torch.empty((rows_q, d.n_q_heads), dtype=torch.float32, device=q.device)
+            if not whole:
+                lse.fill_(-float("inf"))
         elif lse is False or lse is None:
             lse = None
         else:
             assert lse.dtype == torch.float32 and lse.shape == q.shape[:2] and lse.is_contiguous() and lse.device == q.device
-        for s, x in ((d.q_stride, q), (d.k_stride, k), (d.v_stride, v), (d.o_stride, out)):
-            s[0] = x.stride(0) if x.shape[0] > 1 else 0   # (an axis of one element: torch leaves its stride to chance)
-            s[1] = x.stride(1) if x.shape[1] > 1 else 0
-        at = [lens[i].ctypes.data_as(C.POINTER(C.c_int32)) for i in range(4)]
-        _check(lib().tkv_prompt_attn(C.byref(d), q.data_ptr(), k.data_ptr(), v.data_ptr(), out.data_ptr(), _ptr(lse), *at,
+        for i, x in enumerate((q, k, v, out)):
+            st = x.stride()
+            assert st[2] == 1
+            d.strides[2 * i] = st[0] if x.shape[0] > 1 else 0   # (an axis of one element: torch leaves its stride to chance)
+            d.strides[2 * i + 1] = st[1] if x.shape[1] > 1 else 0
+        _check(lib().tkv_prompt_attn(C.byref(d), q.data_ptr(), k.data_ptr(), v.data_ptr(), out.data_ptr(), _ptr(lse), *lens,
                                      float(sm_scale), self.workspace.data_ptr(), self.workspace_bytes, _stream(stream)),
                "tkv_prompt_attn")
         return out if lse is None else (out, lse)

@@ -22,10 +22,13 @@ def L():
 
 
 def _desc(**kw):
-    two = C.c_int64 * 2
-    d = PromptDesc(C.sizeof(PromptDesc), 32, 8, 128, 0, 1, 2, 0, two(4096, 128), two(1024, 128), two(1024, 128), two(4096, 128))
+    d = PromptDesc(C.sizeof(PromptDesc), 32, 8, 128, 0, 1, 2, 0, (C.c_int64 * 8)(4096, 128, 1024, 128, 1024, 128, 4096, 128))
     for key, x in kw.items():
-        setattr(d, key, two(*x) if key.endswith("_stride") else x)
+        if key.endswith("_stride"):
+            i = 2 * "qkvo".index(key[0])
+            d.strides[i], d.strides[i + 1] = x
+        else:
+            setattr(d, key, x)
     return d
 
 

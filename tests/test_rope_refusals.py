@@ -19,11 +19,11 @@ def L():
 
 
 def _call(L, n=3, ptr=None, **kw):
-    d = RopeDesc(C.sizeof(RopeDesc), 32, 8, 128, 0, 0, 1, 1e-6, 128, 0, (C.c_int64 * 2)(6144, 128),
-                 (C.c_int64 * 2)(6144, 128), (C.c_int64 * 2)(6144, 128))
+    d = RopeDesc(C.sizeof(RopeDesc), 32, 8, 128, 0, 0, 1, 1e-6, 128, 0, 6144, 128, 6144, 128, 6144, 128)
     for key, x in kw.items():
         if key.endswith("_stride"):
-            x = (C.c_int64 * 2)(*x)
+            setattr(d, key + "_head", x[1])
+            x = x[0]
         setattr(d, key, x)
     args = dict(q=A, k=A, v=A, positions=A, inv_freq=A, q_weight=A, k_weight=A, q_out=A, k_out=A, v_out=A)
     args.update(ptr or {})
