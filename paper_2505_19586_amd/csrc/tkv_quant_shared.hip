@@ -9,7 +9,10 @@
 //     times code', by two matrix instructions.  The second sum does not depend on the token: sixteen (4 bits: eight) groups at once
 //     are one operand's rows, and the results wait in an LDS table to be added to the logits of a group's blocks as one number.
 //     (K-hat rounded to fp16 would be off by up to 2.7e-3 in outputs where outlier channels are ten times the others.)
-//   * p.V-hat: code s + z is rounded once to fp16, random over the tokens, like the fp16 values it came from.
+//   * p.V-hat at 2 bits: as above, sum_t p[t] (s[t] code'[t]) with an exact product, and sum_t p[t] z[t], sum_t p[t] s[t] of every channel
+//     group as the rows of one more operand.  At 1 and 4 bits code s + z is rounded once to fp16, random over the tokens like the fp16
+//     values it came from (against float64, 131072 tokens: 3.2e-4 of the outputs' norm where rounded, 2.9e-4 where not, of which
+//     2.1e-4 are the outputs' own rounding and as much the weights'; at 4 bits a second part of the scaler would double the products).
 // A wave takes 32-token blocks on its own: the codes lie in the order of the 16x16x32 matrix operands, S^T = K Q^T
 // leaves a query's logits in the lanes where O^T = V^T P^T wants its weights, and nothing is exchanged
 // between lanes but a rare rise of the running maximum.
@@ -199,12 +202,15 @@ __device__ __attribute__((always_inline)) inline void attend(const SharedParams&
   // (Two waves of a SIMD in step wait for the matrix cores and for the vector unit at the same time; with one of them always first they
   // fall out of step: 65.9 -> 64.6 us for 131072 tokens under 16 sequences, 138 -> 134 for 32770 under 64 at 4 bits.)
   if (wave >= kWaves / 2) __builtin_amdgcn_s_setprio(2);
-  floatx4 o[NQ][8];
+  constexpr bool kExactV = BITS == 2;
+  floatx4 o[NQ][8], oz[kExactV ? NQ : 1];  // oz: rows u: weights with zero-points of channel group u, rows 4 + u: with its scalers
   float ref[NQ], sum[NQ];
+  if constexpr (!kExactV) oz[0] = (floatx4){0.f, 0.f, 0.f, 0.f};
 #pragma unroll
   for (int t = 0; t < NQ; ++t) {
     ref[t] = kNone;
     sum[t] = 0.f;
+    if constexpr (kExactV) oz[t] = (floatx4){0.f, 0.f, 0.f, 0.f};
 #pragma unroll
     for (int x = 0; x < 8; ++x) o[t][x] = (floatx4){0.f, 0.f, 0.f, 0.f};
   }
@@ -229,6 +235,7 @@ __device__ __attribute__((always_inline)) inline void attend(const SharedParams&
         sum[t] *= shrink;
 #pragma unroll
         for (int x = 0; x < 8; ++x) o[t][x] *= shrink;
+        if constexpr (kExactV) oz[t] *= shrink;
       }
     }
 #pragma unroll
@@ -245,6 +252,8 @@ __device__ __attribute__((always_inline)) inline void attend(const SharedParams&
     }
   };
 
+  // row col of the operand of zero-points and scalers: zero-points of u = col, scalers of u = col - 4 (rows of no u: whatever is there)
+  const int zs_at = 2 * CB + (col % 8 < 4 ? 768 : 512) + 64 * (col % 4) + 16 * kb;
   uint32_t or_in = 0x64006400u;
   asm("" : "+v"(or_in));
   // The terms of SPAN groups from block j's on: sum_c q[c] (z[c] + c0 s[c]), in units of the exponent.
@@ -358,13 +367,14 @@ __device__ __attribute__((always_inline)) inline void attend(const SharedParams&
     keys(std::integral_constant<int, 3>{});
     constexpr int U = 128 / G;
     uint32_t vw[8];
-    uintx4 vs[U], vz[U];
+    uintx4 vs[U], vz[kExactV ? 1 : U];
     words(at + CB, vw);
 #pragma unroll
     for (int u = 0; u < U; ++u) {
       vs[u] = lds_read16(at + 16 * kb + (2 * CB + 512 + 64 * u));
-      vz[u] = lds_read16(at + 16 * kb + (2 * CB + 768 + 64 * u));
+      if constexpr (!kExactV) vz[u] = lds_read16(at + 16 * kb + (2 * CB + 768 + 64 * u));
     }
+    if constexpr (kExactV) vz[0] = lds_read16(at + zs_at);
     __builtin_amdgcn_sched_barrier(0);
     uintx4 w[NQ];
     soften(s, base, w);
@@ -375,16 +385,25 @@ __device__ __attribute__((always_inline)) inline void attend(const SharedParams&
     auto values = [&](auto X) {  // channels 16 x on
       constexpr int x = decltype(X)::value, u = x * 16 / G;
       half2_t cv[4];
-      codes<BITS, x, 0>(vw, or_in, cv);
+      codes<BITS, x, kExactV ? C0 : 0>(vw, or_in, cv);
       uintx4 v;
 #pragma unroll
       for (int y = 0; y < 4; ++y) {
-        const uint32_t sw = vs[u][y], zw = vz[u][y];
-        v[y] = as_word(__builtin_elementwise_fma(cv[y], as_half2(sw), as_half2(zw)));
+        const uint32_t sw = vs[u][y];
+        if constexpr (kExactV) {
+          v[y] = as_word(cv[y] * as_half2(sw));
+        } else {
+          const uint32_t zw = vz[u][y];
+          v[y] = as_word(__builtin_elementwise_fma(cv[y], as_half2(sw), as_half2(zw)));
+        }
       }
 #pragma unroll
       for (int t = 0; t < NQ; ++t) o[t][x] = mfma(v, w[t], o[t][x]);
     };
+    if constexpr (kExactV) {
+#pragma unroll
+      for (int t = 0; t < NQ; ++t) oz[t] = mfma(vz[0], w[t], oz[t]);
+    }
     values(std::integral_constant<int, 0>{});
     values(std::integral_constant<int, 1>{});
     values(std::integral_constant<int, 2>{});
@@ -442,6 +461,17 @@ __device__ __attribute__((always_inline)) inline void attend(const SharedParams&
 #pragma unroll
       for (int t = 0; t < NQ; ++t) o[t][x] = mfma(v, w[t], o[t][x]);
     }
+  }
+
+  if constexpr (kExactV) {
+#pragma unroll
+    for (int t = 0; t < NQ; ++t)
+#pragma unroll
+      for (int u = 0; u < 128 / G; ++u) {
+        const float zero = __shfl(oz[t][u], col, 64), scale = __shfl(oz[t][u], 16 + col, 64);
+#pragma unroll
+        for (int x = u * G / 16; x < (u + 1) * G / 16; ++x) o[t][x] += zero + C0 * scale;
+      }
   }
 
   // ---- the waves' results joined: references and sums first, then a tile of rows at a time, wave w channels 16 w on
