@@ -121,7 +121,7 @@ template <int BITS, int NQ>
 constexpr int lds_bytes() {
   constexpr int ring = kWaves * kSlots * slot_bytes<BITS>(), q = NQ * 4096, join = (NQ > 1 ? 2 : 1) * kWaves * 8192;
   constexpr int terms = kWaves * span_groups<BITS>() * NQ * 64;
-  return (ring + q + terms > join ? ring + q + terms : join) + kWaves * 16 * NQ * 8;
+  return (ring + q + terms > join ? ring + q + terms : join) + kWaves * 16 * NQ * 8 + 16;
 }
 
 // One segment's rows (16 NQ of them) over one chunk of its tokens.
@@ -134,7 +134,7 @@ __device__ __attribute__((always_inline)) inline void attend(const SharedParams&
   const int lane = threadIdx.x % 64, kb = lane / 16, col = lane % 16;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
   constexpr int kRing = kWaves * kSlots * SB;
-  constexpr int kStats = lds_bytes<BITS, MAXQ>() - kWaves * 16 * MAXQ * 8;
+  constexpr int kStats = lds_bytes<BITS, MAXQ>() - 16 - kWaves * 16 * MAXQ * 8, kOnes = lds_bytes<BITS, MAXQ>() - 16;
   constexpr int SPAN = span_groups<BITS>(), C0 = code_zero<BITS>();
   const lds_at ring = lds0 + wave * kSlots * SB, q_at = lds0 + kRing, stats = lds0 + kStats;
   const lds_at terms = q_at + MAXQ * 4096 + wave * SPAN * NQ * 64;  // [group][tile][16 columns] float32
@@ -197,13 +197,14 @@ __device__ __attribute__((always_inline)) inline void attend(const SharedParams&
     }
     lds_write16(q_at + y * 1024 + 16 * lane, v);
   }
+  if (threadIdx.x == 0) lds_write16(lds0 + kOnes, (uintx4){0x3C003C00u, 0x3C003C00u, 0x3C003C00u, 0x3C003C00u});
   __syncthreads();
 
   // (Two waves of a SIMD in step wait for the matrix cores and for the vector unit at the same time; with one of them always first they
   // fall out of step: 65.9 -> 64.6 us for 131072 tokens under 16 sequences, 138 -> 134 for 32770 under 64 at 4 bits.)
   if (wave >= kWaves / 2) __builtin_amdgcn_s_setprio(2);
   constexpr bool kExactV = BITS == 2;
-  floatx4 o[NQ][8], oz[kExactV ? NQ : 1];  // oz: rows u: weights with zero-points of channel group u, rows 4 + u: with its scalers
+  floatx4 o[NQ][8], oz[kExactV ? NQ : 1];  // oz: row u: weights with zero-points of channel group u, row 4 + u: with its scalers, row 8: the weights' sum
   float ref[NQ], sum[NQ];
   if constexpr (!kExactV) oz[0] = (floatx4){0.f, 0.f, 0.f, 0.f};
 #pragma unroll
@@ -215,7 +216,7 @@ __device__ __attribute__((always_inline)) inline void attend(const SharedParams&
     for (int x = 0; x < 8; ++x) o[t][x] = (floatx4){0.f, 0.f, 0.f, 0.f};
   }
   // logits s, to which base[t] is to be added, to weights
-  auto soften = [&](floatx4 (&s)[2][NQ], const float (&base)[NQ], uintx4 (&w)[NQ]) {
+  auto soften = [&](floatx4 (&s)[2][NQ], const float (&base)[NQ], uintx4 (&w)[NQ], auto Sum) {
     float rise = -INFINITY;
     float top[NQ];
 #pragma unroll
@@ -245,14 +246,14 @@ __device__ __attribute__((always_inline)) inline void attend(const SharedParams&
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
         const float e = __builtin_amdgcn_exp2f(__builtin_fmaf(s[i / 4][t][i % 4], p.scale2, less));
-        sum[t] += e;
+        if constexpr (decltype(Sum)::value) sum[t] += e;
         v[i] = (_Float16)e;
       }
       w[t] = __builtin_bit_cast(uintx4, v);
     }
   };
 
-  // row col of the operand of zero-points and scalers: zero-points of u = col, scalers of u = col - 4 (rows of no u: whatever is there)
+  // row col of the operand of zero-points and scalers: zero-points of u = col, scalers of u = col - 4 (rows of no u: whatever is there), ones
   const int zs_at = 2 * CB + (col % 8 < 4 ? 768 : 512) + 64 * (col % 4) + 16 * kb;
   uint32_t or_in = 0x64006400u;
   asm("" : "+v"(or_in));
@@ -374,10 +375,10 @@ __device__ __attribute__((always_inline)) inline void attend(const SharedParams&
       vs[u] = lds_read16(at + 16 * kb + (2 * CB + 512 + 64 * u));
       if constexpr (!kExactV) vz[u] = lds_read16(at + 16 * kb + (2 * CB + 768 + 64 * u));
     }
-    if constexpr (kExactV) vz[0] = lds_read16(at + zs_at);
+    if constexpr (kExactV) vz[0] = lds_read16(col == 8 ? lds0 + kOnes : at + zs_at);
     __builtin_amdgcn_sched_barrier(0);
     uintx4 w[NQ];
-    soften(s, base, w);
+    soften(s, base, w, std::integral_constant<bool, !kExactV>{});
     asm volatile("s_waitcnt vmcnt(%0)" ::"n"(kLoads) : "memory");  // block j + 1 is there
     words(ring + slot * SB, kw);
     read_channels(0, ring + slot * SB);
@@ -451,7 +452,7 @@ __device__ __attribute__((always_inline)) inline void attend(const SharedParams&
     float base[NQ];
 #pragma unroll
     for (int t = 0; t < NQ; ++t) base[t] = 0.f;
-    soften(s, base, w);
+    soften(s, base, w, std::true_type{});
 #pragma unroll
     for (int x = 0; x < 8; ++x) {
       // tokens 8 kb to 8 kb + 7 of channel 16 x + col: two blocks of four rows, transposed
@@ -478,7 +479,8 @@ __device__ __attribute__((always_inline)) inline void attend(const SharedParams&
   __syncthreads();
 #pragma unroll
   for (int t = 0; t < NQ; ++t) {
-    const float total = tkv::over_rows(sum[t], tkv::SumOf{});
+    float total = tkv::over_rows(sum[t], tkv::SumOf{});
+    if constexpr (kExactV) total += __shfl(oz[t][0], 32 + col, 64);
     if (kb == 0) {
       auto* st = (__attribute__((address_space(3))) float*)(stats + ((t * kWaves + wave) * 16 + col) * 8);
       st[0] = ref[t];
