@@ -9,10 +9,11 @@
 //     times code', by two matrix instructions.  The second sum does not depend on the token: sixteen (4 bits: eight) groups at once
 //     are one operand's rows, and the results wait in an LDS table to be added to the logits of a group's blocks as one number.
 //     (K-hat rounded to fp16 would be off by up to 2.7e-3 in outputs where outlier channels are ten times the others.)
-//   * p.V-hat at 2 bits: as above, sum_t p[t] (s[t] code'[t]) with an exact product, and sum_t p[t] z[t], sum_t p[t] s[t] of every channel
-//     group as the rows of one more operand.  At 1 and 4 bits code s + z is rounded once to fp16, random over the tokens like the fp16
-//     values it came from (against float64, 131072 tokens: 3.2e-4 of the outputs' norm where rounded, 2.9e-4 where not, of which
-//     2.1e-4 are the outputs' own rounding and as much the weights'; at 4 bits a second part of the scaler would double the products).
+//   * p.V-hat likewise: sum_t p[t] (s[t] code'[t]), exact products, and sum_t p[t] z[t], sum_t p[t] s[t] of every channel group and the
+//     weights' own sum as the rows of one more operand.  (V-hat rounded to fp16 takes the outputs' error against float64 from 2.9e-4 of
+//     their norm to 3.5e-4, 2.1e-4 of which is their own rounding; one product instead of two at 4 bits, scaler times code rounded, to
+//     3.4e-4, for 127 us instead of 147 where 64 sequences share 32770 tokens.)  The weights are rounded to fp16, off by at most 2^-11
+//     of each, and divided by the sum of the rounded ones.
 // A wave takes 32-token blocks on its own: the codes lie in the order of the 16x16x32 matrix operands, S^T = K Q^T
 // leaves a query's logits in the lanes where O^T = V^T P^T wants its weights, and nothing is exchanged
 // between lanes but a rare rise of the running maximum.
@@ -117,6 +118,13 @@ template <int BITS>
 constexpr int code_zero() { return BITS == 1 ? 0 : BITS == 2 ? 1 : 8; }  // c0
 template <int BITS>
 constexpr int span_groups() { return BITS == 4 ? 8 : 16; }  // groups whose token-independent terms are worked out at once
+// Two scalers in the parts whose products with codes are exact: at 4 bits the upper eight bits of the significand, then the lower three.
+template <int BITS>
+__device__ inline uint32_t scaler_part(uint32_t w, int part) {
+  if (BITS < 4) return w;
+  const uint32_t high = w & 0xFFF8FFF8u;
+  return part == 0 ? high : as_word(as_half2(w) - as_half2(high));
+}
 template <int BITS, int NQ>
 constexpr int lds_bytes() {
   constexpr int ring = kWaves * kSlots * slot_bytes<BITS>(), q = NQ * 4096, join = (NQ > 1 ? 2 : 1) * kWaves * 8192;
@@ -135,7 +143,7 @@ __device__ __attribute__((always_inline)) inline void attend(const SharedParams&
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
   constexpr int kRing = kWaves * kSlots * SB;
   constexpr int kStats = lds_bytes<BITS, MAXQ>() - 16 - kWaves * 16 * MAXQ * 8, kOnes = lds_bytes<BITS, MAXQ>() - 16;
-  constexpr int SPAN = span_groups<BITS>(), C0 = code_zero<BITS>();
+  constexpr int SPAN = span_groups<BITS>(), C0 = code_zero<BITS>(), kScalerParts = BITS == 4 ? 2 : 1;
   const lds_at ring = lds0 + wave * kSlots * SB, q_at = lds0 + kRing, stats = lds0 + kStats;
   const lds_at terms = q_at + MAXQ * 4096 + wave * SPAN * NQ * 64;  // [group][tile][16 columns] float32
 
@@ -209,15 +217,13 @@ __device__ __attribute__((always_inline)) inline void attend(const SharedParams&
   // (Two waves of a SIMD in step wait for the matrix cores and for the vector unit at the same time; with one of them always first they
   // fall out of step: 65.9 -> 64.6 us for 131072 tokens under 16 sequences, 138 -> 134 for 32770 under 64 at 4 bits.)
   if (wave >= kHalf) __builtin_amdgcn_s_setprio(2);
-  constexpr bool kExactV = BITS == 2;
-  floatx4 o[NQ][8], oz[kExactV ? NQ : 1];  // oz: row u: weights with zero-points of channel group u, row 4 + u: with its scalers, row 8: the weights' sum
+  floatx4 o[NQ][8], oz[NQ];  // oz: row u: weights with zero-points of channel group u, row 4 + u: with its scalers, row 8: the weights' sum
   float ref[NQ], sum[NQ];
-  if constexpr (!kExactV) oz[0] = (floatx4){0.f, 0.f, 0.f, 0.f};
 #pragma unroll
   for (int t = 0; t < NQ; ++t) {
     ref[t] = kNone;
     sum[t] = 0.f;
-    if constexpr (kExactV) oz[t] = (floatx4){0.f, 0.f, 0.f, 0.f};
+    oz[t] = (floatx4){0.f, 0.f, 0.f, 0.f};
 #pragma unroll
     for (int x = 0; x < 8; ++x) o[t][x] = (floatx4){0.f, 0.f, 0.f, 0.f};
   }
@@ -242,7 +248,7 @@ __device__ __attribute__((always_inline)) inline void attend(const SharedParams&
         sum[t] *= shrink;
 #pragma unroll
         for (int x = 0; x < 8; ++x) o[t][x] *= shrink;
-        if constexpr (kExactV) oz[t] *= shrink;
+        oz[t] *= shrink;
       }
     }
 #pragma unroll
@@ -345,15 +351,11 @@ __device__ __attribute__((always_inline)) inline void attend(const SharedParams&
       codes<BITS, m, C0>(kw, or_in, code0);
       codes<BITS, 4 + m, C0>(kw, or_in, code1);
 #pragma unroll
-      for (int part = 0; part < (BITS == 4 ? 2 : 1); ++part) {
+      for (int part = 0; part < kScalerParts; ++part) {
         uintx4 k0, k1;
 #pragma unroll
         for (int y = 0; y < 4; ++y) {
-          uint32_t sw = ks[m % 2][y];
-          if constexpr (BITS == 4) {
-            const uint32_t high = sw & 0xFFF8FFF8u;
-            sw = part == 0 ? high : as_word(as_half2(sw) - as_half2(high));
-          }
+          const uint32_t sw = scaler_part<BITS>(ks[m % 2][y], part);
           k0[y] = as_word(code0[y] * as_half2(sw));
           k1[y] = as_word(code1[y] * as_half2(sw));
         }
@@ -374,17 +376,14 @@ __device__ __attribute__((always_inline)) inline void attend(const SharedParams&
     keys(std::integral_constant<int, 3>{});
     constexpr int U = 128 / G;
     uint32_t vw[8];
-    uintx4 vs[U], vz[kExactV ? 1 : U];
+    uintx4 vs[U], vz;
     words(at + CB, vw);
 #pragma unroll
-    for (int u = 0; u < U; ++u) {
-      vs[u] = lds_read16(at + 16 * kb + (2 * CB + 512 + 64 * u));
-      if constexpr (!kExactV) vz[u] = lds_read16(at + 16 * kb + (2 * CB + 768 + 64 * u));
-    }
-    if constexpr (kExactV) vz[0] = lds_read16(col == 8 ? lds0 + kOnes : at + zs_at);
+    for (int u = 0; u < U; ++u) vs[u] = lds_read16(at + 16 * kb + (2 * CB + 512 + 64 * u));
+    vz = lds_read16(col == 8 ? lds0 + kOnes : at + zs_at);
     __builtin_amdgcn_sched_barrier(0);
     uintx4 w[NQ];
-    soften(s, base, w, std::integral_constant<bool, !kExactV>{});
+    soften(s, base, w, std::false_type{});
     asm volatile("s_waitcnt vmcnt(%0)" ::"n"(kLoads) : "memory");  // block j + 1 is there
     words(ring + slot * SB, kw);
     read_channels(0, ring + slot * SB);
@@ -392,25 +391,18 @@ __device__ __attribute__((always_inline)) inline void attend(const SharedParams&
     auto values = [&](auto X) {  // channels 16 x on
       constexpr int x = decltype(X)::value, u = x * 16 / G;
       half2_t cv[4];
-      codes<BITS, x, kExactV ? C0 : 0>(vw, or_in, cv);
-      uintx4 v;
+      codes<BITS, x, C0>(vw, or_in, cv);
 #pragma unroll
-      for (int y = 0; y < 4; ++y) {
-        const uint32_t sw = vs[u][y];
-        if constexpr (kExactV) {
-          v[y] = as_word(cv[y] * as_half2(sw));
-        } else {
-          const uint32_t zw = vz[u][y];
-          v[y] = as_word(__builtin_elementwise_fma(cv[y], as_half2(sw), as_half2(zw)));
-        }
+      for (int part = 0; part < kScalerParts; ++part) {
+        uintx4 v;
+#pragma unroll
+        for (int y = 0; y < 4; ++y) v[y] = as_word(cv[y] * as_half2(scaler_part<BITS>(vs[u][y], part)));
+#pragma unroll
+        for (int t = 0; t < NQ; ++t) o[t][x] = mfma(v, w[t], o[t][x]);
       }
-#pragma unroll
-      for (int t = 0; t < NQ; ++t) o[t][x] = mfma(v, w[t], o[t][x]);
     };
-    if constexpr (kExactV) {
 #pragma unroll
-      for (int t = 0; t < NQ; ++t) oz[t] = mfma(vz[0], w[t], oz[t]);
-    }
+    for (int t = 0; t < NQ; ++t) oz[t] = mfma(vz, w[t], oz[t]);
     values(std::integral_constant<int, 0>{});
     values(std::integral_constant<int, 1>{});
     values(std::integral_constant<int, 2>{});
@@ -470,23 +462,20 @@ __device__ __attribute__((always_inline)) inline void attend(const SharedParams&
     }
   }
 
-  if constexpr (kExactV) {
 #pragma unroll
-    for (int t = 0; t < NQ; ++t)
+  for (int t = 0; t < NQ; ++t)
 #pragma unroll
-      for (int u = 0; u < 128 / G; ++u) {
-        const float zero = __shfl(oz[t][u], col, 64), scale = __shfl(oz[t][u], 16 + col, 64);
+    for (int u = 0; u < 128 / G; ++u) {
+      const float zero = __shfl(oz[t][u], col, 64), scale = __shfl(oz[t][u], 16 + col, 64);
 #pragma unroll
-        for (int x = u * G / 16; x < (u + 1) * G / 16; ++x) o[t][x] += zero + C0 * scale;
-      }
-  }
+      for (int x = u * G / 16; x < (u + 1) * G / 16; ++x) o[t][x] += zero + C0 * scale;
+    }
 
   // ---- the waves' results joined: references and sums first, then a tile of rows at a time, wave w channels 16 w on
   __syncthreads();
 #pragma unroll
   for (int t = 0; t < NQ; ++t) {
-    float total = tkv::over_rows(sum[t], tkv::SumOf{});
-    if constexpr (kExactV) total += __shfl(oz[t][0], 32 + col, 64);
+    const float total = tkv::over_rows(sum[t], tkv::SumOf{}) + __shfl(oz[t][0], 32 + col, 64);
     if (kb == 0) {
       auto* st = (__attribute__((address_space(3))) float*)(stats + ((t * kWaves + wave) * 16 + col) * 8);
       st[0] = ref[t];
