@@ -58,6 +58,7 @@ struct PromptParams {
   int32_t pieces[TKV_MAX_BATCH];
   int32_t first_row[TKV_MAX_BATCH];   // of the split sequences' rows (of one KV head), for the joining launch
   int32_t tile_rows;                  // rows of a tile: kRows, or kFew
+  int32_t split_rows, most_pieces;
 };
 
 template <typename T>
@@ -516,12 +517,15 @@ __global__ __launch_bounds__(64 * kFewWaves, 1) void prompt_few_kernel(PromptPar
         total == 0.f ? -INFINITY : (top - kShift + __builtin_amdgcn_logf(total)) * 0.69314718055994531f;
 }
 
-// Joins the pieces of the split rows: a workgroup per row, every wave a quarter of the pieces, a lane two channels.
-template <typename T>
+// Joins the pieces of the split rows, a lane two channels.  ONE: a wave per row; otherwise a workgroup, every wave a quarter of the pieces.
+template <typename T, bool ONE>
 __global__ __launch_bounds__(256) void prompt_merge_kernel(PromptParams p) {
   __shared__ float acc_s[4][TKV_D], l_s[4], m_s[4];
   const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
-  const int h = blockIdx.x % p.hkv, at = blockIdx.x / p.hkv;
+  const int item = ONE ? 4 * blockIdx.x + wave : blockIdx.x, first = ONE ? 0 : wave;
+  constexpr int kStep = ONE ? 1 : 4;
+  if (item >= p.split_rows * p.hkv) return;
+  const int h = item % p.hkv, at = item / p.hkv;
   // the last sequence that begins at or before the row (those that are not split share their successor's beginning)
   const bool before = lane < p.batch && p.first_row[min(lane, p.batch - 1)] <= at;
   const int b = __builtin_amdgcn_readfirstlane(__builtin_popcountll(__builtin_amdgcn_ballot_w64(before)) - 1);
@@ -532,11 +536,11 @@ __global__ __launch_bounds__(256) void prompt_merge_kernel(PromptParams p) {
   float m = kNone, l = 0.f;
   float2 acc = make_float2(0.f, 0.f);
   // (requests of eight pieces at a time, absent ones those of the first with a weight of zero)
-  for (int i0 = wave; i0 < pieces; i0 += 32) {
+  for (int i0 = first; i0 < pieces; i0 += 8 * kStep) {
     float2 st[8], v[8];
 #pragma unroll
     for (int y = 0; y < 8; ++y) {
-      const size_t s = slot0 + (i0 + 4 * y < pieces ? i0 + 4 * y : 0) * step;
+      const size_t s = slot0 + (i0 + kStep * y < pieces ? i0 + kStep * y : 0) * step;
       st[y] = *(const float2*)(p.ml + s * 2);
       v[y] = *(const float2*)(p.parts + s * TKV_D + 2 * lane);
     }
@@ -550,11 +554,20 @@ __global__ __launch_bounds__(256) void prompt_merge_kernel(PromptParams p) {
     acc.y *= shrink;
 #pragma unroll
     for (int y = 0; y < 8; ++y) {
-      const float w = i0 + 4 * y < pieces ? __builtin_amdgcn_exp2f(st[y].x - m) : 0.f;
+      const float w = i0 + kStep * y < pieces ? __builtin_amdgcn_exp2f(st[y].x - m) : 0.f;
       l = __builtin_fmaf(st[y].y, w, l);
       acc.x = __builtin_fmaf(v[y].x, w, acc.x);
       acc.y = __builtin_fmaf(v[y].y, w, acc.y);
     }
+  }
+  T* to = (T*)p.out + ((int64_t)(p.seq[b].q_start + token) * p.o_st + (int64_t)(h * p.group + head) * p.o_sh);
+  float* lse = p.lse ? p.lse + ((int64_t)(p.seq[b].q_start + token) * p.hq + h * p.group + head) : nullptr;
+  if constexpr (ONE) {
+    typedef T T2 __attribute__((ext_vector_type(2)));
+    const float inv = l == 0.f ? 0.f : 1.f / l;
+    *(T2*)(to + 2 * lane) = (T2){(T)(acc.x * inv), (T)(acc.y * inv)};
+    if (lse && lane == 0) *lse = l == 0.f ? -INFINITY : (m - kShift + __builtin_amdgcn_logf(l)) * 0.69314718055994531f;
+    return;
   }
   *(float2*)(acc_s[wave] + 2 * lane) = acc;
   if (lane == 0) l_s[wave] = l, m_s[wave] = m;
@@ -569,15 +582,19 @@ __global__ __launch_bounds__(256) void prompt_merge_kernel(PromptParams p) {
     total = __builtin_fmaf(l_s[w], f, total);
     v = __builtin_fmaf(acc_s[w][c], f, v);
   }
-  T* to = (T*)p.out + ((int64_t)(p.seq[b].q_start + token) * p.o_st + (int64_t)(h * p.group + head) * p.o_sh);
   to[c] = (T)(total == 0.f ? 0.f : v / total);
-  if (p.lse && c == 0)
-    p.lse[(int64_t)(p.seq[b].q_start + token) * p.hq + h * p.group + head] =
-        total == 0.f ? -INFINITY : (top - kShift + __builtin_amdgcn_logf(total)) * 0.69314718055994531f;
+  if (lse && c == 0) *lse = total == 0.f ? -INFINITY : (top - kShift + __builtin_amdgcn_logf(total)) * 0.69314718055994531f;
 }
 
+// What the plan goes by, in us: a workgroup's beginning and end and a tile of its keys (64; few rows: 32 for each wave, longer the more
+// workgroups share the memory), and the joining launch with the partial results' way out and back.  Measured with one
+// sequence, 32 query heads, 8 KV heads, whole / in pieces: 512 tokens 22 / 34, 1024 over 1024 35 / 51, 512 over 4096 107 / 56, 333 over 65869
+// 1592 / 377, one over 500 8.5 / 8.8, one over 4000 29.9 / 9.3.
+constexpr double kFixed = 9.5, kTileTime = 1.55, kFewFixed = 5.3, kFewTile = 0.8, kFewLoad = 0.0092;
+constexpr double kJoin = 3, kJoinRow = 3e-4, kJoinPart = 1.7e-4;
+
 template <typename T>
-int32_t launch_prompt(const PromptParams& p, bool few, int32_t items, int32_t split_rows, hipStream_t s) {
+int32_t launch_prompt(const PromptParams& p, bool few, int32_t items, hipStream_t s) {
   const dim3 grid((uint32_t)items * (uint32_t)p.hkv);
   if (few) {
     constexpr int lds = kFewWaves * 4 * kFewKeys * TKV_D * 2;
@@ -589,7 +606,9 @@ int32_t launch_prompt(const PromptParams& p, bool few, int32_t items, int32_t sp
   } else {
     TKV_LAUNCH(prompt_attn_kernel<T>, grid, 64 * kWaves, 0, s, p);
   }
-  if (split_rows) TKV_LAUNCH(prompt_merge_kernel<T>, dim3((uint32_t)split_rows * (uint32_t)p.hkv), 256, 0, s, p);
+  const uint32_t joins = (uint32_t)p.split_rows * (uint32_t)p.hkv;
+  if (joins && p.most_pieces <= 16) TKV_LAUNCH((prompt_merge_kernel<T, true>), dim3((joins + 3) / 4), 256, 0, s, p);
+  else if (joins) TKV_LAUNCH((prompt_merge_kernel<T, false>), dim3(joins), 256, 0, s, p);
   return TKV_OK;
 }
 
@@ -652,8 +671,6 @@ extern "C" int32_t tkv_prompt_attn(const tkv_prompt_desc* d, const void* q, cons
   p.hq = d->n_q_heads; p.hkv = d->n_kv_heads; p.batch = d->batch; p.causal = d->causal;
   p.scale2 = sm_scale * 1.4426950408889634f;
 
-  // Few row tiles: their keys are split into pieces, as many as give every compute unit one workgroup (a workgroup of either
-  // kernel takes most of its compute unit's registers or LDS), of at least four tiles of keys (per wave, where the waves take their own).
   bool few = true;
   for (int b = 0; b < d->batch; ++b) few = few && (int64_t)q_len_host[b] * p.group <= kFew;
   p.tile_rows = few ? kFew : kRows;
@@ -665,31 +682,54 @@ extern "C" int32_t tkv_prompt_attn(const tkv_prompt_desc* d, const void* q, cons
     work += (int64_t)row_tiles(b) * key_tiles(b) * d->n_kv_heads;
     whole += (int64_t)row_tiles(b) * d->n_kv_heads;
   }
-  double per_piece = whole < kWorkgroups ? (double)work / kWorkgroups : 0;
-  if (per_piece > 0 && per_piece < 4) per_piece = 4;
-  int32_t items = 0, parts = 0, split_rows = 0;
-  for (;; per_piece *= 1.05) {
-    items = parts = split_rows = 0;
-    for (int b = 0; b < d->batch; ++b) {
-      p.seq[b] = {q_start_host[b], q_len_host[b], k_start_host[b], k_len_host[b]};
-      int64_t pieces = per_piece > 0 ? (int64_t)((double)key_tiles(b) / per_piece) : 1;
-      if (per_piece > 0 && (double)pieces * per_piece < key_tiles(b)) ++pieces;
-      pieces = pieces < 1 ? 1 : pieces;
-      p.pieces[b] = (int32_t)pieces;
-      p.first_item[b] = items;
-      p.first_part[b] = -1;
-      p.first_row[b] = split_rows;
-      items += row_tiles(b) * p.pieces[b];
-      if (pieces > 1 && row_tiles(b) > 0) {
-        p.first_part[b] = parts;
-        parts += row_tiles(b) * p.pieces[b] * d->n_kv_heads;
-        split_rows += q_len_host[b] * p.group;
+  // Fewer row tiles than compute units (a workgroup of either kernel takes most of its unit's registers or LDS): their keys are
+  // split into pieces of at most `per` tiles, no more workgroups than units, by the size of least estimated time.
+  auto pieces_of = [&](int b, double per) {
+    const int n = key_tiles(b), pieces = (int)(n / per);
+    return pieces * per < n ? pieces + 1 : pieces > 1 ? pieces : 1;
+  };
+  double best = 1e18;
+  if (whole < kWorkgroups) {
+    double least = 0;
+    bool split = true;
+    for (double per = work > kWorkgroups ? (double)work / kWorkgroups : 1; split; per *= 1.15) {  // (at last one piece each)
+      int64_t workgroups = 0, joins = 0, join_parts = 0;
+      int longest = 0;
+      split = false;
+      for (int b = 0; b < d->batch; ++b) {
+        if (!row_tiles(b)) continue;
+        const int n = pieces_of(b, per), most = (key_tiles(b) + n - 1) / n;
+        workgroups += (int64_t)row_tiles(b) * n * d->n_kv_heads;
+        if (most > longest) longest = most;
+        if (n == 1) continue;
+        split = true;
+        joins += (int64_t)q_len_host[b] * d->n_q_heads;
+        join_parts += (int64_t)q_len_host[b] * d->n_q_heads * n;
       }
+      if (workgroups > kWorkgroups) continue;
+      double time = few ? kFewFixed + (kFewTile + kFewLoad * workgroups) * longest : kFixed + kTileTime * longest;
+      if (split) time += kJoin + kJoinRow * joins + kJoinPart * join_parts;
+      if (least == 0 || time < least) least = time, best = per;
     }
-    if (per_piece == 0 || (int64_t)items * d->n_kv_heads <= kWorkgroups) break;  // (at the latest with one piece each)
+  }
+  int32_t items = 0, parts = 0;
+  p.split_rows = p.most_pieces = 0;
+  for (int b = 0; b < d->batch; ++b) {
+    p.seq[b] = {q_start_host[b], q_len_host[b], k_start_host[b], k_len_host[b]};
+    p.pieces[b] = pieces_of(b, best);
+    p.first_item[b] = items;
+    p.first_part[b] = -1;
+    p.first_row[b] = p.split_rows;
+    items += row_tiles(b) * p.pieces[b];
+    if (p.pieces[b] > 1 && row_tiles(b) > 0) {
+      p.first_part[b] = parts;
+      parts += row_tiles(b) * p.pieces[b] * d->n_kv_heads;
+      p.split_rows += q_len_host[b] * p.group;
+      if (p.pieces[b] > p.most_pieces) p.most_pieces = p.pieces[b];
+    }
   }
   p.parts = (float*)workspace;
   p.ml = p.parts + (size_t)kMaxParts * kRows * TKV_D;
   const auto s = (hipStream_t)stream;
-  return d->dtype == TKV_F16 ? launch_prompt<_Float16>(p, few, items, split_rows, s) : launch_prompt<__bf16>(p, few, items, split_rows, s);
+  return d->dtype == TKV_F16 ? launch_prompt<_Float16>(p, few, items, s) : launch_prompt<__bf16>(p, few, items, s);
 }
