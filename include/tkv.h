@@ -228,9 +228,10 @@ int32_t tkv_quant_attn_decode_shared_sizes(const tkv_quant_desc* prefix_desc, co
  * newest tokens stay fp16 as its own descriptor says.
  * prefix_desc and desc: same heads, bits and group_size; residual, capacity and batch may differ.  Either may hold empty
  * sequences; a sequence without any token yields zeros.  q, out: fp16 [B][Hq][128], at multiples of 4 bytes.  sm_scale > 0.
- * All six settings of bits and group_size are evaluated alike: code*s + z rounded to fp16, products of fp16 numbers with float32
- * sums, softmax statistics in float32, its weights rounded to fp16.  Cached values of magnitude up to 30000 are safe (a
- * dequantized value beyond 65504 is infinite).  The result is the same bit for bit from call to call.
+ * All six settings of bits and group_size are evaluated alike: products of codes, scalers and zero-points without a rounding before
+ * the float32 sums, softmax statistics in float32, its weights rounded to fp16.  Cached values of magnitude up to 30000 are safe (a
+ * dequantized value beyond 65504 is infinite).  The result is the same bit for bit from call to call (on streams that may use as
+ * many compute units).
  * Partial results go through `workspace` (16-byte aligned; concurrent calls need separate ones).
  */
 int32_t tkv_quant_attn_decode_shared(const tkv_quant_desc* prefix_desc, const tkv_quant_cache* prefix, const tkv_quant_desc* desc,
@@ -519,9 +520,11 @@ int32_t tkv_prompt_attn_sizes(const tkv_prompt_desc* desc, size_t* workspace_byt
  * lse: float32 [rows of q][Hq] contiguous, the natural logarithm of the sum of exponentials, or NULL.  Rows of out
  * and lse that belong to no sequence are left as they were, rows of k and v behind a sequence's last are not used (whatever they
  * hold).  A non-finite value in a row that a query does not see may still reach it where both lie in the same 64 keys.
- * out must not overlap the inputs; sequences must not share rows of out.  sm_scale > 0 (TKV_E_INVAL otherwise).
+ * out must not overlap the inputs.  Sequences may share keys, in any order, but no row of q and out; sm_scale > 0 (TKV_E_INVAL
+ * otherwise).
  * Products in the inputs' type with float32 sums; softmax statistics and sums in float32, its weights rounded to the
- * inputs' type for the second product.  The result is the same bit for bit from call to call.
+ * inputs' type for the second product.  The result is the same bit for bit from call to call (on streams that may use as
+ * many compute units).
  * Few rows over many keys are split over the keys and joined from partial results in `workspace` (any
  * contents; 16-byte aligned; concurrent calls need separate ones).
  */

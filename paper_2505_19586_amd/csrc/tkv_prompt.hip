@@ -10,6 +10,8 @@
 // LDS reads that transpose 4 x 16 elements on the way.  One pass over the keys: running maximum and
 // sum in float32, weights rounded to the inputs' type for the second product (a relative error of 2^-12 or 2^-9 each, random,
 // beside the output's own rounding of as much).
+#include <algorithm>
+
 #include "tkv_common.h"
 
 namespace {
@@ -26,9 +28,7 @@ typedef __bf16 bhalf8 __attribute__((ext_vector_type(8)));
 constexpr int kKeys = 64;       // keys of a tile
 constexpr int kWaves = 8;
 constexpr int kRows = 32 * kWaves;  // rows of a workgroup
-constexpr int kMaxParts = 256;      // partial results that the workspace has room for
-constexpr int kWorkgroups = 256;     // compute units
-static_assert(kWorkgroups <= kMaxParts, "a split launch's workgroups write a part each");
+constexpr int kMaxParts = 256;      // partial results that the workspace has room for: one per compute unit
 constexpr int kPartFloats = kRows * (TKV_D + 2);
 // Weights are 2^(logit - reference + kShift): the reference follows the running maximum only when a weight is above 2^15, inside
 // fp16's range, and fp16's subnormal numbers begin 2^-21 below the reference's weight, not 2^-14.
@@ -660,9 +660,20 @@ extern "C" int32_t tkv_prompt_attn(const tkv_prompt_desc* d, const void* q, cons
     tiles += ((int64_t)q_len_host[b] * p.group + kRows - 1) / kRows;
     any_keys |= k_len_host[b];
   }
+  // No row of two sequences.  (In order, as nearly always, one look at each says so.)
+  auto q_end = [&](int b) { return q_start_host[b] + q_len_host[b]; };
+  bool in_order = true;
+  for (int b = 0, end = 0; b < d->batch; ++b) {
+    if (q_len_host[b] == 0) continue;
+    in_order = in_order && q_start_host[b] >= end;
+    end = q_end(b);
+  }
+  for (int b = 1; b < d->batch && !in_order; ++b)
+    for (int a = 0; a < b; ++a)
+      if (q_len_host[a] && q_len_host[b] && q_start_host[a] < q_end(b) && q_start_host[b] < q_end(a)) return TKV_E_INVAL;
   if (tiles == 0) return TKV_OK;
   if (!q || !out || (any_keys && (!k || !v))) return TKV_E_INVAL;
-  if (tiles * 2 * d->n_kv_heads > 0x7FFFFFFF) return TKV_E_UNSUPPORTED;
+  if (tiles * d->n_kv_heads >= 1 << 23) return TKV_E_UNSUPPORTED;  // (a launch has fewer than 2^32 threads)
   p.q = q; p.k = k; p.v = v; p.out = out; p.lse = lse;
   p.q_st = d->q_stride[0]; p.q_sh = d->q_stride[1];
   p.k_st = d->k_stride[0]; p.k_sh = d->k_stride[1];
@@ -688,11 +699,13 @@ extern "C" int32_t tkv_prompt_attn(const tkv_prompt_desc* d, const void* q, cons
     const int n = key_tiles(b), pieces = (int)(n / per);
     return pieces * per < n ? pieces + 1 : pieces > 1 ? pieces : 1;
   };
+  const auto s = (hipStream_t)stream;
+  const int units = std::min(kMaxParts, tkv::stream_compute_units(s));
   double best = 1e18;
-  if (whole < kWorkgroups) {
+  if (whole < units) {
     double least = 0;
     bool split = true;
-    for (double per = work > kWorkgroups ? (double)work / kWorkgroups : 1; split; per *= 1.15) {  // (at last one piece each)
+    for (double per = work > units ? (double)work / units : 1; split; per *= 1.15) {  // (at last one piece each)
       int64_t workgroups = 0, joins = 0, join_parts = 0;
       int longest = 0;
       split = false;
@@ -706,7 +719,7 @@ extern "C" int32_t tkv_prompt_attn(const tkv_prompt_desc* d, const void* q, cons
         joins += (int64_t)q_len_host[b] * d->n_q_heads;
         join_parts += (int64_t)q_len_host[b] * d->n_q_heads * n;
       }
-      if (workgroups > kWorkgroups) continue;
+      if (workgroups > units) continue;
       double time = few ? kFewFixed + (kFewTile + kFewLoad * workgroups) * longest : kFixed + kTileTime * longest;
       if (split) time += kJoin + kJoinRow * joins + kJoinPart * join_parts;
       if (least == 0 || time < least) least = time, best = per;
@@ -730,6 +743,5 @@ extern "C" int32_t tkv_prompt_attn(const tkv_prompt_desc* d, const void* q, cons
   }
   p.parts = (float*)workspace;
   p.ml = p.parts + (size_t)kMaxParts * kRows * TKV_D;
-  const auto s = (hipStream_t)stream;
   return d->dtype == TKV_F16 ? launch_prompt<_Float16>(p, few, items, s) : launch_prompt<__bf16>(p, few, items, s);
 }

@@ -20,6 +20,8 @@
 //
 // Prefix and own tokens are split over workgroups in proportion to their cost; partial (reference, sum, weighted V) results
 // go through the workspace to a second launch that joins them.
+#include <algorithm>
+
 #include "tkv_common.h"
 
 namespace {
@@ -606,7 +608,7 @@ __global__ __launch_bounds__(256) void shared_merge_kernel(SharedParams p) {
 // trip, the join of its waves); measured at 2 bits.
 constexpr double block_cost(int nq) { return nq == 1 ? 200 : nq == 2 ? 300 : 464; }
 constexpr double fixed_cost(int nq) { return nq == 1 ? 6000 : nq == 2 ? 8000 : 10000; }
-constexpr int kWorkgroups = 256;  // workgroups at a time: one per compute unit (it takes most of the LDS)
+constexpr int kWorkgroups = 256;  // workgroups at a time, at most: one per compute unit (it takes most of the LDS)
 
 int tiles_of(int rows) { return rows <= 16 ? 1 : rows <= 32 ? 2 : 4; }
 
@@ -735,7 +737,9 @@ extern "C" int32_t tkv_quant_attn_decode_shared(const tkv_quant_desc* pd, const 
     const int64_t fill = (blocks + kWaves - 1) / kWaves;
     return (int32_t)(n < fill ? n : fill);
   };
-  const double even = all / kWorkgroups > 1 ? all / kWorkgroups : 1;
+  const auto s = (hipStream_t)stream;
+  const int units = std::min(kWorkgroups, tkv::stream_compute_units(s));
+  const double even = all / units > 1 ? all / units : 1;
   double best = even, least = 0;
   for (double per = even; per < 4 * even && per < 1.2 * (double)longest * block_cost(tiles) + 1; per *= 1.12) {
     double n_prefix = 0, n_own = 0, long_prefix = 0, long_own = 0, sum = 0;
@@ -755,8 +759,8 @@ extern "C" int32_t tkv_quant_attn_decode_shared(const tkv_quant_desc* pd, const 
       sum += each * n * p.hkv;
       if (each > long_own) long_own = each;
     }
-    double time = (double)(int64_t)((n_prefix + kWorkgroups - 1) / kWorkgroups) * long_prefix;
-    const double shared_out = sum / kWorkgroups + (n_prefix + n_own > kWorkgroups ? long_own / 2 : 0);
+    double time = (double)(int64_t)((n_prefix + units - 1) / units) * long_prefix;
+    const double shared_out = sum / units + (n_prefix + n_own > units ? long_own / 2 : 0);
     if (shared_out > time) time = shared_out;
     if (long_own > time) time = long_own;
     if (least == 0 || time < least) least = time, best = per;
@@ -784,7 +788,6 @@ extern "C" int32_t tkv_quant_attn_decode_shared(const tkv_quant_desc* pd, const 
   }
   if (slots > slots_max) return TKV_E_WORKSPACE;  // (cannot be)
 
-  const auto s = (hipStream_t)stream;
   int32_t r = TKV_OK;
   if (items) {
     const int key = 10 * d->bits + d->group_size / 32;

@@ -196,6 +196,7 @@ extern "C" int32_t tkv_qk_norm_rope(const tkv_rope_desc* d, int32_t n_tokens, co
   // 4096 17.9 / 17.4 / 16.8, 32768 140 / 136 / 149.)
   p.per_wave = (int64_t)n_tokens * octets >= 6000 ? 2 : 1;
   p.parts = (octets + p.per_wave - 1) / p.per_wave;
+  if ((int64_t)n_tokens * p.parts > 4 * ((1 << 24) - 1)) return TKV_E_UNSUPPORTED;  // (a launch has fewer than 2^32 threads)
   p.pairs8 = d->rotary_dim / 16;
   p.interleaved = d->interleaved; p.norm = d->norm; p.eps = d->eps;
   const auto s = (hipStream_t)stream;

@@ -55,6 +55,17 @@ def test_refusals(L, kw, status):
     assert _call(L, **kw) == status
 
 
+@pytest.mark.parametrize("starts,lens,status", [
+    ((0, 4), (5, 5), -1), ((4, 0), (5, 5), -1), ((3, 3), (1, 1), -1), ((0, 2), (5, 1), -1), ((2, 0), (1, 5), -1),
+])
+def test_no_row_belongs_to_two_sequences(L, starts, lens, status):
+    assert _call(L, lens=(starts, lens, (0, 5), (5, 5))) == status
+
+
+def test_more_rows_than_a_launch_has_workgroups(L):
+    assert _call(L, lens=((0, 1 << 29), (1 << 27, 5), (0, 5), (5, 5)), n_q_heads=64, n_kv_heads=64) == -2
+
+
 def test_sizes(L):
     n = C.c_size_t()
     assert L.tkv_prompt_attn_sizes(C.byref(_desc()), C.byref(n)) == 0 and n.value > 0

@@ -44,5 +44,9 @@ def test_refusals(L, kw, status):
     assert _call(L, **kw) == status
 
 
+def test_more_tokens_than_a_launch_has_waves(L):
+    assert _call(L, n=(1 << 31) - 1, n_q_heads=1, n_kv_heads=1) == -2
+
+
 def test_null_descriptor(L):
     assert L.tkv_qk_norm_rope(None, 1, *([A] * 10), None) == -1
