@@ -176,6 +176,70 @@ def test_side_stream_replayed_graph_and_shared_workspace():
         q += 0.25
 
 
+def test_stream_argument_orders_new_outputs():
+    """New outputs are made on the stream that writes them, whatever the current one is busy with."""
+    print("case stream argument", flush=True)
+    q, k, v = _rows(40, 8, torch.float16, 53), _rows(40, 2, torch.float16, 54), _rows(40, 2, torch.float16, 55)
+    plan = tkv.PromptAttention(n_q_heads=8, n_kv_heads=2)
+    want, want_lse = plan.attend(q, k, v, SM, [33], [33], lse=True)
+    side, busy = torch.cuda.Stream(), torch.zeros(1 << 28, device="cuda")
+    torch.cuda.synchronize()
+    for stream in (side, side.cuda_stream):
+        for _ in range(20):
+            busy += 1
+        got, lse = plan.attend(q, k, v, SM, [33], [33], lse=True, stream=stream)
+        torch.cuda.synchronize()
+        assert torch.equal(want, got) and torch.equal(want_lse, lse) and not got[33:].any()
+
+
+def test_sequences_that_share_keys_in_any_order():
+    print("case shared keys", flush=True)
+    q, k, v = _rows(90, 8, torch.float16, 56), _rows(200, 2, torch.float16, 57), _rows(200, 2, torch.float16, 58)
+    plan = tkv.PromptAttention(n_q_heads=8, n_kv_heads=2, batch=3)
+    out = plan.attend(q, k, v, SM, [30, 0, 50], [200, 7, 150], q_starts=[60, 10, 0], k_starts=[0, 0, 50])
+    _compare(out[60:], None, q[60:], k, v, True, torch.float16)
+    _compare(out[:50], None, q[:50], k[50:], v[50:], True, torch.float16)
+    assert not out[50:60].any()
+    with pytest.raises(tkv.TkvError):
+        plan.attend(q, k, v, SM, [30, 0, 50], [200, 7, 150], q_starts=[49, 10, 0], k_starts=[0, 0, 50])
+
+
+@pytest.mark.parametrize("dtype", [torch.float16, torch.bfloat16])
+@pytest.mark.parametrize("q_lens,k_lens", [([256], [3000]), ([300, 1, 20], [5000, 700, 20]), ([1, 8], [9000, 40]), ([2], [70000])])
+def test_split_keys(q_lens, k_lens, dtype):
+    """Both kernels with their keys in pieces, joined by a wave per row and (more than 16 pieces) by a workgroup."""
+    print(f"case split {q_lens} {k_lens} {dtype}", flush=True)
+    _run(q_lens, k_lens, 8, 2, dtype, seed=sum(q_lens))
+
+
+def test_stream_with_compute_unit_mask():
+    """On part of the machine the keys are split into fewer pieces."""
+    import ctypes as C
+    print("case masked stream", flush=True)
+    hip = C.CDLL("libamdhip64.so")
+    create = hip.hipExtStreamCreateWithCUMask
+    create.argtypes = [C.POINTER(C.c_void_p), C.c_uint32, C.POINTER(C.c_uint32)]
+    create.restype = C.c_int
+    mask = (C.c_uint32 * 8)(0xFFFF0000, 0xFFFFFFFF, 0xFFFFFFFF, 0x0000FFFF, 0, 0, 0, 0)   # 96 units
+    handle = C.c_void_p()
+    if create(C.byref(handle), 8, mask) != 0 or not handle.value:
+        pytest.skip("streams with a compute-unit mask are not available")
+    try:
+        q, k, v = _rows(70, 8, torch.float16, 63), _rows(6000, 2, torch.float16, 64), _rows(6000, 2, torch.float16, 65)
+        plan = tkv.PromptAttention(n_q_heads=8, n_kv_heads=2)
+        torch.cuda.synchronize()
+        for n in (70, 3):
+            out = torch.empty_like(q[:n])
+            torch.cuda.synchronize()
+            plan.attend(q[:n], k, v, SM, [n], [6000], out=out, stream=torch.cuda.ExternalStream(handle.value))
+            torch.cuda.synchronize()
+            _compare(out, None, q[:n], k, v, True, torch.float16)
+    finally:
+        torch.cuda.synchronize()
+        hip.hipStreamDestroy.argtypes = [C.c_void_p]
+        hip.hipStreamDestroy(handle)
+
+
 def test_large_offsets():
     """Sequences that begin beyond 2^31 elements of a tensor."""
     print("case large offsets", flush=True)

@@ -176,6 +176,23 @@ def test_side_stream_and_replayed_graph():
         q *= 0.75
 
 
+def test_one_layer_as_prefix_and_batch_and_two_plans_at_once():
+    """A layer may continue itself; two plans (a workspace each) run on two streams at the same time."""
+    print("case same layer, two streams", flush=True)
+    L, inps = _fill([500, 90], 8, 2, 2, 32, 128, 5)
+    rows = [_rows(i, 2, 32, 128) for i in inps]
+    q = torch.from_numpy(np.stack([i.q for i in inps])).cuda()
+    plans = [tkv.SharedPrefix(L, L) for _ in range(2)]
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    torch.cuda.synchronize()
+    outs = [[p.attn_decode(q, SM, prefix_of=of, stream=s) for p, s, of in zip(plans, streams, ([1, 0], [-1, 1]))] for _ in range(8)]
+    torch.cuda.synchronize()
+    for a, b in outs:
+        _check(a, q, rows, rows, [1, 0])
+        _check(b, q, rows, rows, [-1, 1])
+        assert torch.equal(a, outs[0][0]) and torch.equal(b, outs[0][1])
+
+
 @pytest.mark.parametrize("bits,group,hq,hkv,batch,n", [(2, 32, 32, 8, 16, 131072), (1, 64, 64, 8, 40, 40001)])
 def test_long_prefixes(bits, group, hq, hkv, batch, n):
     """Long prefixes against float64 on the GPU, of rows drawn there; values centred and not."""
