@@ -8,8 +8,13 @@
 // one number per lane (two lanes share a row), and its weights already lie where O^T = V^T P^T wants them: the sixteen
 // keys that a lane's weights belong to are read in that order on the V side (a sum over keys does not mind their order), by
 // LDS reads that transpose 4 x 16 elements on the way.  One pass over the keys: running maximum and
-// sum in float32, weights rounded to the inputs' type for the second product (a relative error of 2^-12 or 2^-9 each, random,
-// beside the output's own rounding of as much).
+// sum in float32, weights rounded to the inputs' type for the second product (off by at most 2^-11 or 2^-8 of each, random over
+// the keys, beside the output's own rounding of as much: against float64 2.6e-4 of the outputs' norm in fp16, 2.1e-4 of them the latter).
+//
+// Long prompts are bound by the LDS reads beside the matrix products (a wave reads a tile's keys and values, 32 KiB, for 32 rows; 64
+// bytes a clock and compute unit: as long as the products of both) and by the clock, which falls to 1.6-1.8 GHz under them: 32 query
+// heads over 8, causal: 4096 tokens 147 us (933 TFLOP/s), 16384 2095 us (1050; the same products alone 1553 us, without the LDS reads
+// 1770).  64 rows a wave would halve the reads but spilled 69 registers.
 #include <algorithm>
 
 #include "tkv_common.h"
@@ -117,9 +122,9 @@ __device__ inline Item find_item(const PromptParams& p, int it) {
   return x;
 }
 
-// A wave's work on a tile of 64 keys is two products on the matrix cores and the softmax between them on the vector units, about
-// 1024 and 900 cycles.  Two waves of a SIMD left to themselves fall into step and wait for the same unit, so the workgroup's two halves
-// (waves 0 to 3 and 4 to 7: one of each on every SIMD) take turns: while one multiplies (the weights of its last tile with the
+// A wave's work on a tile of 64 keys is two products on the matrix cores, 1024 cycles, and the softmax between them on the vector
+// units, about 900.  Two waves of a SIMD left to themselves fall into step and wait for the same unit, so the workgroup's two halves
+// (waves 0 to 3 and 4 to 7: one of each on every SIMD) take turns (16384 tokens: 2267 -> 2110 us): while one multiplies (the weights of its last tile with the
 // values, the queries with the next keys), the other works out weights, and a barrier changes the parts.
 template <typename T>
 __global__ __launch_bounds__(64 * kWaves, 2) void prompt_attn_kernel(PromptParams p) {
@@ -348,6 +353,9 @@ __global__ __launch_bounds__(64 * kWaves, 2) void prompt_attn_kernel(PromptParam
 
 // Few rows (single tokens, a few tokens of few heads: up to 32 of a sequence and KV head).  The keys' bytes bound this:
 // every wave takes 32-key tiles of its own through a ring of two of its own, with no barrier until the waves join.
+// (Single tokens of four sequences, 201 MB of keys and values: 34 us, 5.9 TB/s, and 4 us for the join.  With this kernel / with the one
+// above, 32 query heads over 8: a token over 500 keys 8.5 / 11.5 us, 8 over 32768 of four sequences 101 / 111, 4 over 2000 of 64 95 / 103;
+// a token over 32768 28.4 / 27.8.)
 constexpr int kFew = 32, kFewWaves = 4, kFewKeys = 32;
 
 template <typename T>
@@ -518,6 +526,8 @@ __global__ __launch_bounds__(64 * kFewWaves, 1) void prompt_few_kernel(PromptPar
 }
 
 // Joins the pieces of the split rows, a lane two channels.  ONE: a wave per row; otherwise a workgroup, every wave a quarter of the pieces.
+// (Whole calls with a workgroup / a wave per row: 1024 rows of 32 heads in 2 pieces 81 / 51 us, 333 rows in 12 389 / 377; one row of 32
+// heads in 32 pieces with a workgroup 9.1.)
 template <typename T, bool ONE>
 __global__ __launch_bounds__(256) void prompt_merge_kernel(PromptParams p) {
   __shared__ float acc_s[4][TKV_D], l_s[4], m_s[4];

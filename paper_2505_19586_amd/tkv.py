@@ -3,7 +3,6 @@ marshalling only.  Every step of the path runs in the library's HIP kernels; the
 is no CPU or PyTorch fallback - a missing library or GPU raises."""
 from __future__ import annotations
 
-import contextlib
 import ctypes as C
 import itertools
 import operator
@@ -180,11 +179,12 @@ def _on_current(t: torch.Tensor, stream) -> None:
         f"tensors on {t.device}, the current device is another: make it current or pass a stream of theirs"
 
 
-def _made_on(stream, device):
-    """Where new outputs are made: in the order of the stream that will write them."""
-    if stream is None:
-        return contextlib.nullcontext()
-    return torch.cuda.stream(stream if hasattr(stream, "cuda_stream") else torch.cuda.ExternalStream(int(stream), device=device))
+def _new(shape, dtype, device, stream, fill=None) -> torch.Tensor:
+    """A new output, made (and filled) in the order of the stream that will write it."""
+    if stream is not None:
+        with torch.cuda.stream(stream if hasattr(stream, "cuda_stream") else torch.cuda.ExternalStream(int(stream), device=device)):
+            return _new(shape, dtype, device, None, fill)
+    return torch.empty(shape, dtype=dtype, device=device) if fill is None else torch.full(shape, fill, dtype=dtype, device=device)
 
 
 def _ptr(t) -> int:
@@ -324,8 +324,7 @@ class SharedPrefix:
             of = np.ascontiguousarray(prefix_of, dtype=np.int32)
             assert of.shape == (d.batch,)
         if out is None:
-            with _made_on(stream, q.device):
-                out = torch.empty_like(q)
+            out = _new(q.shape, q.dtype, q.device, stream)
         else:
             assert out.dtype == torch.float16 and out.is_contiguous() and out.shape == q.shape and out.device == q.device
         _check(lib().tkv_quant_attn_decode_shared(C.byref(self.prefix.desc), C.byref(self.prefix.cache), C.byref(d),
@@ -622,13 +621,12 @@ def qk_norm_rope(q: torch.Tensor, k: torch.Tensor, positions: torch.Tensor | Non
         out_dtype = next((x.dtype for x in (q_out, k_out, v_out) if x is not None), dt)
     for x, o in ((q, q_out), (k, k_out), (v, v_out)):
         assert o is None or (x is not None and o.dtype == out_dtype and o.shape == x.shape and o.is_contiguous() and o.device == dev)
-    with _made_on(stream, dev):
-        if q_out is None:
-            q_out = torch.empty((t, hq, ch), dtype=out_dtype, device=dev)
-        if k_out is None:
-            k_out = torch.empty((t, hkv, ch), dtype=out_dtype, device=dev)
-        if v_out is None and v is not None:
-            v_out = torch.empty((t, hkv, ch), dtype=out_dtype, device=dev)
+    if q_out is None:
+        q_out = _new((t, hq, ch), out_dtype, dev, stream)
+    if k_out is None:
+        k_out = _new((t, hkv, ch), out_dtype, dev, stream)
+    if v_out is None and v is not None:
+        v_out = _new((t, hkv, ch), out_dtype, dev, stream)
     # (an axis of one element: torch leaves its stride to chance)
     by_t, by_q, by_k = t > 1, hq > 1, hkv > 1
     desc = RopeDesc(C.sizeof(RopeDesc), hq, hkv, ch, _DTYPES.get(dt, -1), _DTYPES.get(out_dtype, -1), norm, eps, rot, interleaved,
@@ -683,15 +681,11 @@ class PromptAttention:
         lens = [(C.c_int32 * n)(*x) for x in (begin(q_starts, q_lens, rows_q, "q_starts"), q_lens,
                                               begin(k_starts, k_lens, rows_k, "k_starts"), k_lens)]
         if out is None:
-            with _made_on(stream, q.device):
-                out = (torch.empty if whole else torch.zeros)(q.shape, dtype=q.dtype, device=q.device)
+            out = _new(q.shape, q.dtype, q.device, stream, None if whole else 0.0)
         else:
             assert out.dtype == q.dtype and out.shape == q.shape and out.device == q.device
         if lse is True:
-            with _made_on(stream, q.device):
-                lse = torch.empty((rows_q, d.n_q_heads), dtype=torch.float32, device=q.device)
-                if not whole:
-                    lse.fill_(-float("inf"))
+            lse = _new((rows_q, d.n_q_heads), torch.float32, q.device, stream, None if whole else -float("inf"))
         elif lse is False or lse is None:
             lse = None
         else:
