@@ -175,7 +175,7 @@ def _stream(stream) -> int:
 
 def _on_current(t: torch.Tensor, stream) -> None:
     """Without a stream the current device's is used: the tensors have to be that device's."""
-    assert stream is not None or t.device.index == torch._C._cuda_getDevice(), \
+    assert stream is not None or t.get_device() == torch._C._cuda_getDevice(), \
         f"tensors on {t.device}, the current device is another: make it current or pass a stream of theirs"
 
 
@@ -599,28 +599,28 @@ def qk_norm_rope(q: torch.Tensor, k: torch.Tensor, positions: torch.Tensor | Non
     """tkv_qk_norm_rope: q [T, Hq, 128], k, v [T, Hkv, 128] (fp16 or bf16, views of one fused projection
     allowed), positions int32 [T], inv_freq float32 [R/2] (None: no rotation) -> contiguous (q_out, k_out, v_out or
     None) in out_dtype (default: the inputs')."""
-    t, hq, ch = q.shape
-    t2, hkv, ch2 = k.shape
-    dt, dev = q.dtype, q.device
-    assert q.is_cuda and t2 == t and ch2 == ch and k.dtype == dt and k.device == dev
+    t, hq, ch = shape_q = q.shape
+    t2, hkv, ch2 = shape_k = k.shape
+    dt, dev, at = q.dtype, q.device, q.get_device()  # (numbers of devices compare in a third of the time of devices)
+    assert q.is_cuda and t2 == t and ch2 == ch and k.dtype == dt and k.get_device() == at
     _on_current(q, stream)
     sq, sk, sv = q.stride(), k.stride(), (0, 0, 1)
     if v is not None:
-        assert v.shape == k.shape and v.dtype == dt and v.device == dev
+        assert v.shape == shape_k and v.dtype == dt and v.get_device() == at
         sv = v.stride()
     assert sq[2] == 1 and sk[2] == 1 and sv[2] == 1
     rot = 0
     if inv_freq is not None:
-        assert inv_freq.dtype == torch.float32 and inv_freq.dim() == 1 and inv_freq.is_contiguous() and inv_freq.device == dev
-        assert positions is not None and positions.dtype == torch.int32 and positions.device == dev
+        assert inv_freq.dtype == torch.float32 and inv_freq.dim() == 1 and inv_freq.is_contiguous() and inv_freq.get_device() == at
+        assert positions is not None and positions.dtype == torch.int32 and positions.get_device() == at
         assert positions.shape == (t,) and positions.is_contiguous()
         rot = 2 * inv_freq.shape[0]
     for w in (q_weight, k_weight):
-        assert w is None or (w.shape == (ch,) and w.is_contiguous() and w.dtype == dt and w.device == dev)
+        assert w is None or (w.shape == (ch,) and w.is_contiguous() and w.dtype == dt and w.get_device() == at)
     if out_dtype is None:
         out_dtype = next((x.dtype for x in (q_out, k_out, v_out) if x is not None), dt)
-    for x, o in ((q, q_out), (k, k_out), (v, v_out)):
-        assert o is None or (x is not None and o.dtype == out_dtype and o.shape == x.shape and o.is_contiguous() and o.device == dev)
+    for o, shape in ((q_out, shape_q), (k_out, shape_k), (v_out, shape_k if v is not None else None)):
+        assert o is None or (o.dtype == out_dtype and o.shape == shape and o.is_contiguous() and o.get_device() == at)
     if q_out is None:
         q_out = _new((t, hq, ch), out_dtype, dev, stream)
     if k_out is None:
