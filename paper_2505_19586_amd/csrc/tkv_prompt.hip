@@ -710,7 +710,7 @@ extern "C" int32_t tkv_prompt_attn(const tkv_prompt_desc* d, const void* q, cons
     return pieces * per < n ? pieces + 1 : pieces > 1 ? pieces : 1;
   };
   const auto s = (hipStream_t)stream;
-  const int units = std::min(kMaxParts, tkv::stream_compute_units(s));
+  const int units = work > whole ? std::min(kMaxParts, tkv::stream_compute_units(s)) : 0;  // (0: nothing to split)
   double best = 1e18;
   if (whole < units) {
     double least = 0;

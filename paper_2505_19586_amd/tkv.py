@@ -125,10 +125,10 @@ def lib() -> C.CDLL:
         L.tkv_classify_layer.argtypes = [C.POINTER(C.c_float), i32, i32, C.c_float, C.POINTER(C.c_float)]
         L.tkv_qk_norm_rope.argtypes = [C.POINTER(RopeDesc), i32] + [vp] * 11
         L.tkv_prompt_attn_sizes.argtypes = [C.POINTER(PromptDesc), C.POINTER(sz)]
-        L.tkv_prompt_attn.argtypes = [C.POINTER(PromptDesc)] + [vp] * 5 + [C.POINTER(i32)] * 4 + [C.c_float, vp, sz, vp]
+        L.tkv_prompt_attn.argtypes = [C.POINTER(PromptDesc)] + [vp] * 9 + [C.c_float, vp, sz, vp]
         L.tkv_quant_attn_decode_shared_sizes.argtypes = [C.POINTER(QuantDesc), C.POINTER(QuantDesc), C.POINTER(sz)]
         L.tkv_quant_attn_decode_shared.argtypes = [C.POINTER(QuantDesc), C.POINTER(QuantCache), C.POINTER(QuantDesc),
-                                                   C.POINTER(QuantCache), C.POINTER(i32), vp, vp, C.c_float, vp, sz, vp]
+                                                   C.POINTER(QuantCache), vp, vp, vp, C.c_float, vp, sz, vp]
         L.tkv_debug_quant_attn_config.argtypes = [i32, i32]
         L.tkv_debug_quant_attn_config.restype = i32
         L.tkv_debug_read_sweep.argtypes = [vp, C.c_size_t, vp, i32, vp]
@@ -323,13 +323,14 @@ class SharedPrefix:
         if prefix_of is not None:
             of = np.ascontiguousarray(prefix_of, dtype=np.int32)
             assert of.shape == (d.batch,)
+            of_at = of.__array_interface__["data"][0]
         if out is None:
             out = _new(q.shape, q.dtype, q.device, stream)
         else:
             assert out.dtype == torch.float16 and out.is_contiguous() and out.shape == q.shape and out.device == q.device
         _check(lib().tkv_quant_attn_decode_shared(C.byref(self.prefix.desc), C.byref(self.prefix.cache), C.byref(d),
                                                   C.byref(self.layer.cache),
-                                                  None if of is None else of.ctypes.data_as(C.POINTER(C.c_int32)), q.data_ptr(),
+                                                  None if of is None else of_at, q.data_ptr(),
                                                   out.data_ptr(), float(sm_scale), self.workspace.data_ptr(), self.workspace_bytes,
                                                   _stream(stream)), "tkv_quant_attn_decode_shared")
         return out
@@ -651,6 +652,7 @@ class PromptAttention:
         self.dtype = dtype
         self.device = dev
         self._q_row, self._k_row = (n_q_heads, head_dim), (n_kv_heads, head_dim)
+        self._strides, self._ints, self._lens_bytes = self.desc.strides, C.c_int32 * (4 * batch), 4 * batch
 
     def attend(self, q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, sm_scale: float, q_lens, k_lens=None, *,
                q_starts=None, k_starts=None, out: torch.Tensor | None = None, lse: bool | torch.Tensor = False, stream=None):
@@ -662,11 +664,12 @@ class PromptAttention:
         d, n = self.desc, self.desc.batch
         rows_q, rows_k = q.shape[0], k.shape[0]
         assert q.is_cuda and k.shape == v.shape and q.shape[1:] == self._q_row and k.shape[1:] == self._k_row
-        assert q.dtype == k.dtype == v.dtype == self.dtype and q.device == k.device == v.device == self.workspace.device
+        assert q.dtype == k.dtype == v.dtype == self.dtype
+        assert q.get_device() == k.get_device() == v.get_device() == self.workspace.get_device()
         _on_current(q, stream)
 
         def ints(x, what):
-            x = [int(i) for i in x]
+            x = [*map(int, x)]
             assert len(x) == n and min(x) >= 0, f"{what}: {n} numbers, none below 0"
             return x
 
@@ -678,8 +681,8 @@ class PromptAttention:
         q_lens = ints(q_lens, "q_lens")
         k_lens = q_lens if k_lens is None else ints(k_lens, "k_lens")
         whole = q_starts is None and sum(q_lens) == rows_q  # every row is some sequence's
-        lens = [(C.c_int32 * n)(*x) for x in (begin(q_starts, q_lens, rows_q, "q_starts"), q_lens,
-                                              begin(k_starts, k_lens, rows_k, "k_starts"), k_lens)]
+        lens = self._ints(*begin(q_starts, q_lens, rows_q, "q_starts"), *q_lens, *begin(k_starts, k_lens, rows_k, "k_starts"), *k_lens)
+        by = self._lens_bytes
         if out is None:
             out = _new(q.shape, q.dtype, q.device, stream, None if whole else 0.0)
         else:
@@ -690,13 +693,13 @@ class PromptAttention:
             lse = None
         else:
             assert lse.dtype == torch.float32 and lse.shape == q.shape[:2] and lse.is_contiguous() and lse.device == q.device
-        for i, x in enumerate((q, k, v, out)):
-            st = x.stride()
-            assert st[2] == 1
-            d.strides[2 * i] = st[0] if x.shape[0] > 1 else 0   # (an axis of one element: torch leaves its stride to chance)
-            d.strides[2 * i + 1] = st[1] if x.shape[1] > 1 else 0
-        _check(lib().tkv_prompt_attn(C.byref(d), q.data_ptr(), k.data_ptr(), v.data_ptr(), out.data_ptr(), _ptr(lse), *lens,
-                                     float(sm_scale), self.workspace.data_ptr(), self.workspace_bytes, _stream(stream)),
+        (qt, qh, qc), (kt, kh, kc), (vt, vh, vc), (ot, oh, oc) = q.stride(), k.stride(), v.stride(), out.stride()
+        assert qc == kc == vc == oc == 1
+        # (an axis of one element: torch leaves its stride to chance)
+        by_q, by_k, by_qh, by_kh = rows_q > 1, rows_k > 1, d.n_q_heads > 1, d.n_kv_heads > 1
+        self._strides[:] = (by_q * qt, by_qh * qh, by_k * kt, by_kh * kh, by_k * vt, by_kh * vh, by_q * ot, by_qh * oh)
+        _check(lib().tkv_prompt_attn(C.byref(d), q.data_ptr(), k.data_ptr(), v.data_ptr(), out.data_ptr(), _ptr(lse), lens, C.byref(lens, by),
+                                     C.byref(lens, 2 * by), C.byref(lens, 3 * by), float(sm_scale), self.workspace.data_ptr(), self.workspace_bytes, _stream(stream)),
                "tkv_prompt_attn")
         return out if lse is None else (out, lse)
 
