@@ -525,7 +525,7 @@ int32_t tkv_prompt_attn_sizes(const tkv_prompt_desc* desc, size_t* workspace_byt
  * Products in the inputs' type with float32 sums; softmax statistics and sums in float32, its weights rounded to the
  * inputs' type for the second product.  The result is the same bit for bit from call to call (on streams that may use as
  * many compute units).
- * Few rows over many keys are split over the keys and joined from partial results in `workspace` (any
+ * Few rows, and sequences far longer than the others, are split over the keys and joined from partial results in `workspace` (any
  * contents; 16-byte aligned; concurrent calls need separate ones).
  */
 int32_t tkv_prompt_attn(const tkv_prompt_desc* desc, const void* q, const void* k, const void* v, void* out, float* lse,

@@ -699,24 +699,30 @@ extern "C" int32_t tkv_prompt_attn(const tkv_prompt_desc* d, const void* q, cons
   auto key_tiles = [&](int b) { return (k_len_host[b] + keys - 1) / keys; };
   auto row_tiles = [&](int b) { return (q_len_host[b] * p.group + p.tile_rows - 1) / p.tile_rows; };
   int64_t work = 0, whole = 0;
+  int most_tiles = 0;
   for (int b = 0; b < d->batch; ++b) {
     work += (int64_t)row_tiles(b) * key_tiles(b) * d->n_kv_heads;
     whole += (int64_t)row_tiles(b) * d->n_kv_heads;
+    if (row_tiles(b) && key_tiles(b) > most_tiles) most_tiles = key_tiles(b);
   }
-  // Fewer row tiles than compute units (a workgroup of either kernel takes most of its unit's registers or LDS): their keys are
-  // split into pieces of at most `per` tiles, no more workgroups than units, by the size of least estimated time.
+  // A row tile whose keys are more than a compute unit's even share (a workgroup of either kernel takes most of its unit's registers
+  // or LDS): keys are split into pieces of at most `per` tiles, by the size of least estimated time.  Fewer row tiles than units
+  // stay one round of workgroups.  (One token of each of 33 sequences, 65536 keys and 32 times 100: 560 us whole, 55 in pieces; 41 prompts of
+  // 40 x 64 and 200 tokens, the latter over 40000 keys: 980, 176.)
   auto pieces_of = [&](int b, double per) {
     const int n = key_tiles(b), pieces = (int)(n / per);
     return pieces * per < n ? pieces + 1 : pieces > 1 ? pieces : 1;
   };
   const auto s = (hipStream_t)stream;
-  const int units = work > whole ? std::min(kMaxParts, tkv::stream_compute_units(s)) : 0;  // (0: nothing to split)
+  const int units = most_tiles > 1 ? std::min(kMaxParts, tkv::stream_compute_units(s)) : 1;
+  const int64_t max_parts = kMaxParts * (kRows / p.tile_rows);
   double best = 1e18;
-  if (whole < units) {
+  const double share = work > units ? (double)work / units : 1;
+  if (most_tiles > share) {
     double least = 0;
     bool split = true;
-    for (double per = work > units ? (double)work / units : 1; split; per *= 1.15) {  // (at last one piece each)
-      int64_t workgroups = 0, joins = 0, join_parts = 0;
+    for (double per = share; split; per *= 1.15) {  // (at last one piece each)
+      int64_t workgroups = 0, joins = 0, join_parts = 0, parts = 0;
       int longest = 0;
       split = false;
       for (int b = 0; b < d->batch; ++b) {
@@ -726,11 +732,14 @@ extern "C" int32_t tkv_prompt_attn(const tkv_prompt_desc* d, const void* q, cons
         if (most > longest) longest = most;
         if (n == 1) continue;
         split = true;
+        parts += (int64_t)row_tiles(b) * n * d->n_kv_heads;
         joins += (int64_t)q_len_host[b] * d->n_q_heads;
         join_parts += (int64_t)q_len_host[b] * d->n_q_heads * n;
       }
-      if (workgroups > units) continue;
-      double time = few ? kFewFixed + (kFewTile + kFewLoad * workgroups) * longest : kFixed + kTileTime * longest;
+      if (parts > max_parts || (whole <= units && workgroups > units)) continue;
+      const double tiles_each = longest > share ? longest : share, rounds = (double)((workgroups + units - 1) / units);
+      const double tile_time = few ? kFewTile + kFewLoad * (workgroups < units ? workgroups : units) : kTileTime;
+      double time = (few ? kFewFixed : kFixed) * rounds + tile_time * tiles_each;
       if (split) time += kJoin + kJoinRow * joins + kJoinPart * join_parts;
       if (least == 0 || time < least) least = time, best = per;
     }

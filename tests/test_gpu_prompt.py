@@ -212,6 +212,14 @@ def test_split_keys(q_lens, k_lens, dtype):
     _run(q_lens, k_lens, 8, 2, dtype, seed=sum(q_lens))
 
 
+@pytest.mark.parametrize("q_lens,k_lens", [([1] * 40, [7000] + [90] * 39), ([1] * 63 + [8], [5] * 62 + [0, 30000]),
+                                           ([9] + [1] * 35 + [0], [9000] + [200] * 35 + [50]), ([40] * 40 + [70], [40] * 40 + [12000])])
+def test_long_sequences_among_many(q_lens, k_lens):
+    """More row tiles than compute units (8 KV heads), one sequence far above the even share: that one is split."""
+    print(f"case ragged {len(q_lens)} sequences, {max(k_lens)} keys", flush=True)
+    _run(q_lens, k_lens, 16, 8, torch.float16, seed=len(q_lens))
+
+
 def test_stream_with_compute_unit_mask():
     """On part of the machine the keys are split into fewer pieces."""
     import ctypes as C
