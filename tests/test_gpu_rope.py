@@ -101,6 +101,21 @@ def test_outputs_over_their_inputs_and_heads_in_another_order():
     assert got[0] is q and all(torch.equal(a, b) for a, b in zip(got, want))
 
 
+@pytest.mark.parametrize("t,hq,hkv", [(1501, 32, 4), (6100, 3, 1), (2000, 40, 8)])
+def test_long_outputs_over_their_inputs(t, hq, hkv):
+    """Enough rows for waves of two octets, also with an odd number of them."""
+    q, k, v, qw, kw = _inputs(t, hq, hkv, torch.bfloat16, seed=t, fused=False)
+    pos, f = torch.arange(t, device="cuda", dtype=torch.int32), _freq(64)
+    want = tkv.qk_norm_rope(q, k, pos, f, v=v, norm=True, q_weight=qw, k_weight=kw)
+    some = [0, t // 2, t - 1]
+    _check(want[0][some], q[some], pos[some], f, torch.bfloat16, norm=True, weight=qw.double().cpu().numpy())
+    _check(want[1][some], k[some], pos[some], f, torch.bfloat16, norm=True, weight=kw.double().cpu().numpy())
+    short = tkv.qk_norm_rope(q[-40:], k[-40:], pos[-40:], f, v=v[-40:], norm=True, q_weight=qw, k_weight=kw)
+    assert all(torch.equal(a[-40:], b) for a, b in zip(want, short))
+    got = tkv.qk_norm_rope(q, k, pos, f, v=v, norm=True, q_weight=qw, k_weight=kw, q_out=q, k_out=k, v_out=v)
+    assert all(torch.equal(a, b) for a, b in zip(got, want))
+
+
 def test_no_tokens():
     q, k, v, _, _ = _inputs(0, 32, 8, torch.float16)
     out = tkv.qk_norm_rope(q, k, torch.zeros(0, dtype=torch.int32, device="cuda"), _freq(128), v=v)

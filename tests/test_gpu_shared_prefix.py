@@ -3,8 +3,8 @@ from one sequence to 64, prefixes of any length, none and several, rings that wr
 replayed graphs and a run from a prompt's rows to shared decoding.
 
 Tolerance: the framework's measure of attention outputs (max over heads of max_c |o - ref| / max_c |ref|) and its bound
-of 2e-3: dequantized values, weights and outputs are fp16 numbers, 2^-11 relative each at most; a key's rounding
-(2^-11 of the value, random over 128 channels) moves a logit by about 2^-12 of its size."""
+of 2e-3: weights and outputs are fp16 numbers, off by at most 2^-11 = 4.9e-4 of each; codes, scalers and zero-points enter the
+products unrounded, sums are float32."""
 import numpy as np
 import pytest
 import torch
