@@ -233,7 +233,7 @@ __device__ __attribute__((always_inline)) inline void attend(const SharedParams&
 #pragma unroll
     for (int x = 0; x < 8; ++x) o[t][x] = (floatx4){0.f, 0.f, 0.f, 0.f};
   }
-  // logits s, to which base[t] is to be added, to weights
+  // logits s, to which base[t] is to be added, to weights; Sum: the rounded weights are added up here, not by the operand's row of ones
   auto soften = [&](floatx4 (&s)[2][NQ], const float (&base)[NQ], uintx4 (&w)[NQ], auto Sum) {
     float rise = -INFINITY;
     float top[NQ];
@@ -264,8 +264,8 @@ __device__ __attribute__((always_inline)) inline void attend(const SharedParams&
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
         const float e = __builtin_amdgcn_exp2f(__builtin_fmaf(s[i / 4][t][i % 4], p.scale2, less));
-        if constexpr (decltype(Sum)::value) sum[t] += e;
         v[i] = (_Float16)e;
+        if constexpr (decltype(Sum)::value) sum[t] += (float)v[i];
       }
       w[t] = __builtin_bit_cast(uintx4, v);
     }
