@@ -520,8 +520,9 @@ int32_t tkv_prompt_attn_sizes(const tkv_prompt_desc* desc, size_t* workspace_byt
  * lse: float32 [rows of q][Hq] contiguous, the natural logarithm of the sum of exponentials, or NULL.  Rows of out
  * and lse that belong to no sequence are left as they were, rows of k and v behind a sequence's last are not used (whatever they
  * hold).  A non-finite value in a row that a query does not see may still reach it where both lie in the same 64 keys.
- * out must not overlap the inputs.  Sequences may share keys, in any order, but no row of q and out; sm_scale > 0 (TKV_E_INVAL
- * otherwise).
+ * Addresses are multiples of 16 bytes (lse: 4).  out must not overlap the inputs.  Sequences may share keys, in any order, but no row
+ * of q and out; rows of out, one for every head of the tokens from the first to the last of the call, must not overlap (those of q, k
+ * and v may: strides of 0); sm_scale > 0 (TKV_E_INVAL otherwise).
  * Products in the inputs' type with float32 sums; softmax statistics and sums in float32, its weights rounded to the
  * inputs' type for the second product.  The result is the same bit for bit from call to call (on streams that may use as
  * many compute units).

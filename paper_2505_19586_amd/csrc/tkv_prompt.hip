@@ -637,6 +637,19 @@ bool good_strides(const int64_t* s) {
   return s[0] >= 0 && s[1] >= 0 && s[0] % 8 == 0 && s[1] % 8 == 0 && s[0] <= (1 << 22) && s[1] <= ((int64_t)1 << 40);
 }
 
+// Whether no two rows of 128 elements overlap, one at every t s[0] + h s[1].
+bool rows_apart(const int64_t* s, int64_t tokens, int64_t heads) {
+  if (tokens == 0) return true;
+  if ((tokens > 1 && s[0] < TKV_D) || (heads > 1 && s[1] < TKV_D)) return false;
+  // heads within a token, or tokens within a head: all but strides made by hand
+  if (tokens == 1 || heads == 1 || s[0] >= (heads - 1) * s[1] + TKV_D || s[1] >= (tokens - 1) * s[0] + TKV_D) return true;
+  for (int64_t h = 1; h < heads; ++h) {  // the two tokens whose rows lie next to those h heads on
+    const int64_t t = h * s[1] / s[0], r = h * s[1] % s[0];
+    if ((t < tokens && r < TKV_D) || (t + 1 < tokens && s[0] - r < TKV_D)) return false;
+  }
+  return true;
+}
+
 }  // namespace
 
 extern "C" int32_t tkv_prompt_attn_sizes(const tkv_prompt_desc* d, size_t* workspace_bytes) {
@@ -656,19 +669,18 @@ extern "C" int32_t tkv_prompt_attn(const tkv_prompt_desc* d, const void* q, cons
   if (!q_start_host || !q_len_host || !k_start_host || !k_len_host || !workspace) return TKV_E_INVAL;
   if (!(sm_scale > 0.f) || !(sm_scale <= 3.402823466e38f)) return TKV_E_INVAL;
   if (!good_strides(d->q_stride) || !good_strides(d->k_stride) || !good_strides(d->v_stride) || !good_strides(d->o_stride)) return TKV_E_INVAL;
-  if (workspace_bytes < (size_t)kMaxParts * kPartFloats * sizeof(float)) return TKV_E_WORKSPACE;
-  for (const void* x : {q, k, v, (const void*)out, (const void*)workspace})
-    if (((uintptr_t)x & 15) != 0) return TKV_E_INVAL;
-  if (((uintptr_t)lse & 3) != 0) return TKV_E_INVAL;
   PromptParams p;
   p.group = d->n_q_heads / d->n_kv_heads;
-  int64_t tiles = 0, any_keys = 0;
+  int64_t tiles = 0, any_keys = 0, q_first = 0, q_last = 0;  // (rows of out: from q_first on, q_last not among them)
   for (int b = 0; b < d->batch; ++b) {
     if (q_start_host[b] < 0 || q_len_host[b] < 0 || k_start_host[b] < 0 || k_len_host[b] < 0) return TKV_E_INVAL;
     if ((int64_t)q_len_host[b] * p.group > (1 << 30) || k_len_host[b] > (1 << 30)) return TKV_E_UNSUPPORTED;
     if ((int64_t)q_start_host[b] + q_len_host[b] > 0x7FFFFFFF || (int64_t)k_start_host[b] + k_len_host[b] > 0x7FFFFFFF) return TKV_E_INVAL;
     tiles += ((int64_t)q_len_host[b] * p.group + kRows - 1) / kRows;
     any_keys |= k_len_host[b];
+    if (q_len_host[b] == 0) continue;
+    if (q_last == 0 || q_start_host[b] < q_first) q_first = q_start_host[b];
+    q_last = std::max<int64_t>(q_last, q_start_host[b] + q_len_host[b]);
   }
   // No row of two sequences.  (In order, as nearly always, one look at each says so.)
   auto q_end = [&](int b) { return q_start_host[b] + q_len_host[b]; };
@@ -681,6 +693,11 @@ extern "C" int32_t tkv_prompt_attn(const tkv_prompt_desc* d, const void* q, cons
   for (int b = 1; b < d->batch && !in_order; ++b)
     for (int a = 0; a < b; ++a)
       if (q_len_host[a] && q_len_host[b] && q_start_host[a] < q_end(b) && q_start_host[b] < q_end(a)) return TKV_E_INVAL;
+  if (!rows_apart(d->o_stride, q_last - q_first, d->n_q_heads)) return TKV_E_INVAL;
+  if (workspace_bytes < (size_t)kMaxParts * kPartFloats * sizeof(float)) return TKV_E_WORKSPACE;
+  for (const void* x : {q, k, v, (const void*)out, (const void*)workspace})
+    if (((uintptr_t)x & 15) != 0) return TKV_E_INVAL;
+  if (((uintptr_t)lse & 3) != 0) return TKV_E_INVAL;
   if (tiles == 0) return TKV_OK;
   if (!q || !out || (any_keys && (!k || !v))) return TKV_E_INVAL;
   if (tiles * d->n_kv_heads >= 1 << 23) return TKV_E_UNSUPPORTED;  // (a launch has fewer than 2^32 threads)

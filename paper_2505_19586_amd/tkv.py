@@ -658,7 +658,7 @@ class PromptAttention:
                q_starts=None, k_starts=None, out: torch.Tensor | None = None, lse: bool | torch.Tensor = False, stream=None):
         """q [Tq, Hq, 128], k, v [Tk, Hkv, 128] (views of wider rows allowed); q_lens, k_lens (default: q_lens): tokens of
         every sequence, one after the other unless q_starts / k_starts say where each begins (sequences may share keys, not
-        queries).  Returns out
+        queries).  out: [Tq, Hq, 128], a view too, but not one whose rows overlap.  Returns out
         [Tq, Hq, 128], or (out, lse [Tq, Hq]) where lse is True or a float32 tensor.  Rows of no sequence are left as they
         were (a new out has zeros there)."""
         d, n = self.desc, self.desc.batch
