@@ -499,7 +499,7 @@ typedef struct {
   int32_t dtype;        /* tkv_dtype of q, k, v and out                                   */
   int32_t causal;       /* 1: a token sees the keys up to its own; 0: all of its sequence */
   int32_t batch;        /* sequences, 1..TKV_MAX_BATCH                                    */
-  int32_t reserved;     /* 0                                                              */
+  int32_t reserved;     /* 0 (TKV_E_INVAL otherwise)                                      */
   int64_t q_stride[2];  /* strides of tokens and heads in elements, multiples of 8, that of */
   int64_t k_stride[2];  /* tokens at most 2^22; the 128 channels of a row lie side by side  */
   int64_t v_stride[2];

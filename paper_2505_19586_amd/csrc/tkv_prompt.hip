@@ -627,7 +627,7 @@ int32_t check_prompt_desc(const tkv_prompt_desc* d) {
   if (d->n_q_heads <= 0 || d->n_kv_heads <= 0 || d->head_dim <= 0 || d->batch <= 0) return TKV_E_INVAL;
   if (d->n_q_heads % d->n_kv_heads != 0) return TKV_E_INVAL;
   if (d->dtype != TKV_F16 && d->dtype != TKV_BF16) return TKV_E_INVAL;
-  if (d->causal != 0 && d->causal != 1) return TKV_E_INVAL;
+  if ((d->causal != 0 && d->causal != 1) || d->reserved != 0) return TKV_E_INVAL;
   if (d->head_dim != TKV_D || d->batch > TKV_MAX_BATCH || d->n_q_heads > 1024) return TKV_E_UNSUPPORTED;
   return TKV_OK;
 }

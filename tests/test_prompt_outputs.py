@@ -1,4 +1,4 @@
-"""tkv_prompt_attn refuses outputs whose rows overlap, before any GPU work (no GPU needed)."""
+"""tkv_prompt_attn refuses outputs whose rows overlap and a reserved field that is not 0, before any GPU work (no GPU needed)."""
 import pytest
 
 from test_prompt_refusals import L, _call  # noqa: F401  (the library, a call on addresses that are never read)
@@ -40,3 +40,6 @@ def test_rows_apart_as_counted_one_by_one(L):  # noqa: F811
         assert _call(L, lens=lens, n_q_heads=heads, n_kv_heads=1, o_stride=(st, sh), ws=16) == (-4 if apart else -1), (heads, n, st, sh)
         seen.add(apart)
     assert seen == {True, False}
+
+def test_reserved(L):  # noqa: F811
+    assert _call(L, reserved=1, ws=16) == -1
