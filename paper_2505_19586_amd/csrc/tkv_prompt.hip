@@ -693,6 +693,7 @@ extern "C" int32_t tkv_prompt_attn(const tkv_prompt_desc* d, const void* q, cons
   for (int b = 1; b < d->batch && !in_order; ++b)
     for (int a = 0; a < b; ++a)
       if (q_len_host[a] && q_len_host[b] && q_start_host[a] < q_end(b) && q_start_host[b] < q_end(a)) return TKV_E_INVAL;
+  if (tiles * d->n_kv_heads >= 1 << 23) return TKV_E_UNSUPPORTED;  // (a launch has fewer than 2^32 threads)
   if (!rows_apart(d->o_stride, q_last - q_first, d->n_q_heads)) return TKV_E_INVAL;
   if (workspace_bytes < (size_t)kMaxParts * kPartFloats * sizeof(float)) return TKV_E_WORKSPACE;
   for (const void* x : {q, k, v, (const void*)out, (const void*)workspace})
@@ -700,7 +701,6 @@ extern "C" int32_t tkv_prompt_attn(const tkv_prompt_desc* d, const void* q, cons
   if (((uintptr_t)lse & 3) != 0) return TKV_E_INVAL;
   if (tiles == 0) return TKV_OK;
   if (!q || !out || (any_keys && (!k || !v))) return TKV_E_INVAL;
-  if (tiles * d->n_kv_heads >= 1 << 23) return TKV_E_UNSUPPORTED;  // (a launch has fewer than 2^32 threads)
   p.q = q; p.k = k; p.v = v; p.out = out; p.lse = lse;
   p.q_st = d->q_stride[0]; p.q_sh = d->q_stride[1];
   p.k_st = d->k_stride[0]; p.k_sh = d->k_stride[1];
