@@ -652,7 +652,7 @@ class PromptAttention:
         self.dtype = dtype
         self.device = dev
         self._q_row, self._k_row = (n_q_heads, head_dim), (n_kv_heads, head_dim)
-        self._strides, self._ints, self._lens_bytes = self.desc.strides, C.c_int32 * (4 * batch), 4 * batch
+        self._ints, self._lens_bytes = C.c_int32 * (4 * batch), 4 * batch
 
     def attend(self, q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, sm_scale: float, q_lens, k_lens=None, *,
                q_starts=None, k_starts=None, out: torch.Tensor | None = None, lse: bool | torch.Tensor = False, stream=None):
@@ -697,7 +697,8 @@ class PromptAttention:
         assert qc == kc == vc == oc == 1
         # (an axis of one element: torch leaves its stride to chance)
         by_q, by_k, by_qh, by_kh = rows_q > 1, rows_k > 1, d.n_q_heads > 1, d.n_kv_heads > 1
-        self._strides[:] = (by_q * qt, by_qh * qh, by_k * kt, by_kh * kh, by_k * vt, by_kh * vh, by_q * ot, by_qh * oh)
+        d = PromptDesc.from_buffer_copy(d)  # (this call's strides: another thread's call may be in the library with its own)
+        d.strides[:] = (by_q * qt, by_qh * qh, by_k * kt, by_kh * kh, by_k * vt, by_kh * vh, by_q * ot, by_qh * oh)
         _check(lib().tkv_prompt_attn(C.byref(d), q.data_ptr(), k.data_ptr(), v.data_ptr(), out.data_ptr(), _ptr(lse), lens, C.byref(lens, by),
                                      C.byref(lens, 2 * by), C.byref(lens, 3 * by), float(sm_scale), self.workspace.data_ptr(), self.workspace_bytes, _stream(stream)),
                "tkv_prompt_attn")
