@@ -7,6 +7,7 @@ import ctypes as C
 import itertools
 import operator
 import os
+import threading
 
 import numpy as np
 import torch
@@ -187,6 +188,28 @@ def _new(shape, dtype, device, stream, fill=None) -> torch.Tensor:
     return torch.empty(shape, dtype=dtype, device=device) if fill is None else torch.full(shape, fill, dtype=dtype, device=device)
 
 
+class _Workspaces:
+    """The workspaces of an object's calls: one for every stream, whose calls follow each other, and one of its own for every call made
+    while the current stream is captured into a graph (it stays in the graph's memory pool), as graphs may be replayed beside each
+    other and beside eager calls.  Threads hold `lock` while their call's launches go out, so that none of another thread's, with
+    the same workspace, comes in between."""
+
+    def __init__(self, n_bytes: int, device: torch.device):
+        self._bytes, self._device, self._of = n_bytes, device, {}
+        self.lock = threading.Lock()
+        with torch.cuda.device(device):
+            self.of(_stream(None))
+
+    def of(self, handle: int, stream=None) -> torch.Tensor:
+        captured = torch._C._cuda_isCurrentStreamCapturing()
+        w = None if captured else self._of.get(handle)
+        if w is None:
+            w = _new(self._bytes, torch.uint8, self._device, stream)
+            if not captured:
+                self._of[handle] = w
+        return w
+
+
 def _ptr(t) -> int:
     return 0 if t is None else t.data_ptr()
 
@@ -302,7 +325,8 @@ class QuantLayer:
 class SharedPrefix:
     """Decode attention of a batch (`layer`) whose sequences share prefixes, each held once in `prefix`
     (tkv_quant_attn_decode_shared).  Both are ordinary QuantLayers: append a prompt to `prefix`, every sequence's own
-    tokens to `layer`."""
+    tokens to `layer`.  Streams, threads and captured graphs may use one object at the same time (each stream and graph has a workspace
+    of its own); a graph keeps the numbers of tokens that it was captured with."""
 
     def __init__(self, prefix: QuantLayer, layer: QuantLayer):
         ws = C.c_size_t()
@@ -311,13 +335,19 @@ class SharedPrefix:
         assert prefix.workspace.device == layer.workspace.device
         self.prefix, self.layer = prefix, layer
         self.workspace_bytes = int(ws.value)
-        self.workspace = torch.empty(self.workspace_bytes, dtype=torch.uint8, device=layer.device)
+        self._device = layer.workspace.device
+        self._workspaces = _Workspaces(self.workspace_bytes, self._device)
+
+    @property
+    def workspace(self) -> torch.Tensor:
+        """That of the current stream's calls."""
+        return self._workspaces.of(_stream(None))
 
     def attn_decode(self, q: torch.Tensor, sm_scale: float, prefix_of=None, out: torch.Tensor | None = None, stream=None):
         """q fp16 [B, Hq, 128]; prefix_of: for every sequence the prefix it continues, -1 for none (default: 0 for all)."""
         d = self.layer.desc
         assert q.dtype == torch.float16 and q.is_contiguous() and tuple(q.shape) == (d.batch, d.n_q_heads, d.head_dim)
-        assert q.device == self.workspace.device
+        assert q.device == self._device
         _on_current(q, stream)
         of = None
         if prefix_of is not None:
@@ -328,11 +358,14 @@ class SharedPrefix:
             out = _new(q.shape, q.dtype, q.device, stream)
         else:
             assert out.dtype == torch.float16 and out.is_contiguous() and out.shape == q.shape and out.device == q.device
-        _check(lib().tkv_quant_attn_decode_shared(C.byref(self.prefix.desc), C.byref(self.prefix.cache), C.byref(d),
-                                                  C.byref(self.layer.cache),
-                                                  None if of is None else of_at, q.data_ptr(),
-                                                  out.data_ptr(), float(sm_scale), self.workspace.data_ptr(), self.workspace_bytes,
-                                                  _stream(stream)), "tkv_quant_attn_decode_shared")
+        handle = _stream(stream)
+        with self._workspaces.lock:
+            workspace = self._workspaces.of(handle, stream)
+            status = lib().tkv_quant_attn_decode_shared(C.byref(self.prefix.desc), C.byref(self.prefix.cache), C.byref(d),
+                                                        C.byref(self.layer.cache), None if of is None else of_at, q.data_ptr(),
+                                                        out.data_ptr(), float(sm_scale), workspace.data_ptr(), self.workspace_bytes,
+                                                        handle)
+        _check(status, "tkv_quant_attn_decode_shared")
         return out
 
 
@@ -639,7 +672,8 @@ def qk_norm_rope(q: torch.Tensor, k: torch.Tensor, positions: torch.Tensor | Non
 
 
 class PromptAttention:
-    """Attention over whole prompts, packed sequences and chunks (tkv_prompt_attn): the workspace and the call."""
+    """Attention over whole prompts, packed sequences and chunks (tkv_prompt_attn): the workspaces and the call.  Streams, threads and
+    captured graphs may use one object at the same time (each stream and graph has a workspace of its own, 32.5 MiB)."""
 
     def __init__(self, *, n_q_heads=32, n_kv_heads=8, head_dim=128, dtype=torch.float16, causal=True, batch=1,
                  device="cuda:0"):
@@ -648,11 +682,17 @@ class PromptAttention:
         ws = C.c_size_t()
         _check(lib().tkv_prompt_attn_sizes(C.byref(self.desc), C.byref(ws)), "tkv_prompt_attn_sizes")
         self.workspace_bytes = int(ws.value)
-        self.workspace = torch.empty(self.workspace_bytes, dtype=torch.uint8, device=dev)
+        self._at = torch.cuda.current_device() if dev.index is None else dev.index
+        self._workspaces = _Workspaces(self.workspace_bytes, torch.device("cuda", self._at))
         self.dtype = dtype
         self.device = dev
         self._q_row, self._k_row = (n_q_heads, head_dim), (n_kv_heads, head_dim)
         self._ints, self._lens_bytes = C.c_int32 * (4 * batch), 4 * batch
+
+    @property
+    def workspace(self) -> torch.Tensor:
+        """That of the current stream's calls."""
+        return self._workspaces.of(_stream(None))
 
     def attend(self, q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, sm_scale: float, q_lens, k_lens=None, *,
                q_starts=None, k_starts=None, out: torch.Tensor | None = None, lse: bool | torch.Tensor = False, stream=None):
@@ -665,7 +705,7 @@ class PromptAttention:
         rows_q, rows_k = q.shape[0], k.shape[0]
         assert q.is_cuda and k.shape == v.shape and q.shape[1:] == self._q_row and k.shape[1:] == self._k_row
         assert q.dtype == k.dtype == v.dtype == self.dtype
-        assert q.get_device() == k.get_device() == v.get_device() == self.workspace.get_device()
+        assert q.get_device() == k.get_device() == v.get_device() == self._at
         _on_current(q, stream)
 
         def ints(x, what):
@@ -699,9 +739,13 @@ class PromptAttention:
         by_q, by_k, by_qh, by_kh = rows_q > 1, rows_k > 1, d.n_q_heads > 1, d.n_kv_heads > 1
         d = PromptDesc.from_buffer_copy(d)  # (this call's strides: another thread's call may be in the library with its own)
         d.strides[:] = (by_q * qt, by_qh * qh, by_k * kt, by_kh * kh, by_k * vt, by_kh * vh, by_q * ot, by_qh * oh)
-        _check(lib().tkv_prompt_attn(C.byref(d), q.data_ptr(), k.data_ptr(), v.data_ptr(), out.data_ptr(), _ptr(lse), lens, C.byref(lens, by),
-                                     C.byref(lens, 2 * by), C.byref(lens, 3 * by), float(sm_scale), self.workspace.data_ptr(), self.workspace_bytes, _stream(stream)),
-               "tkv_prompt_attn")
+        handle = _stream(stream)
+        with self._workspaces.lock:
+            workspace = self._workspaces.of(handle, stream)
+            status = lib().tkv_prompt_attn(C.byref(d), q.data_ptr(), k.data_ptr(), v.data_ptr(), out.data_ptr(), _ptr(lse), lens,
+                                           C.byref(lens, by), C.byref(lens, 2 * by), C.byref(lens, 3 * by), float(sm_scale),
+                                           workspace.data_ptr(), self.workspace_bytes, handle)
+        _check(status, "tkv_prompt_attn")
         return out if lse is None else (out, lse)
 
 
