@@ -40,7 +40,7 @@ constexpr int kPartFloats = kRows * (TKV_D + 2);
 constexpr float kShift = 7.f;
 template <typename T>
 constexpr uint32_t too_large() { return __is_same(T, _Float16) ? 0x7800u : 0x4700u; }  // 2^15's bits
-constexpr float kNone = -1e30f;  // reference of a row without a key so far
+constexpr float kNone = -3.402823466e38f;  // reference of a row without a key so far (finite: kNone - kNone is 0)
 
 struct PromptSeq {
   int32_t q_start, q_len, k_start, k_len;
