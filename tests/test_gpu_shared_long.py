@@ -42,19 +42,32 @@ def _rows(batch, n, hkv, gen):
     return k, v + 0.5
 
 
+def _part(q, k, v):
+    """Rows' largest logits, sums of exponentials and weighted values over one stretch of tokens (none: -inf, 0, 0)."""
+    if len(k) == 0:
+        return q.new_full((len(q), 1), -float("inf")), q.new_zeros(len(q), 1), q.new_zeros(len(q), 128)
+    s = q @ k.T.contiguous() * SM
+    m = s.amax(1, keepdim=True)
+    w = torch.exp(s - m)
+    return m, w.sum(1, keepdim=True), w @ v
+
+
 def _check(out, q, prefix, own, lens, of, bits, group, hkv):
-    """prefix, own: (k, v) [B, n, Hkv, 128]; of: every sequence's prefix, -1: none."""
-    grp, worst = q.shape[1] // hkv, 0.0
+    """prefix, own: (k, v) [B, n, Hkv, 128]; of: every sequence's prefix, -1: none.  Each prefix once for all of its sequences."""
+    grp, batch, worst = q.shape[1] // hkv, len(lens), 0.0
     for h in range(hkv):
-        ps = [_dequantized(prefix[0][i, :, h], prefix[1][i, :, h], bits, group) for i in range(len(prefix[0]))]
-        for b in range(len(lens)):
-            k, v = _dequantized(own[0][b, :lens[b], h], own[1][b, :lens[b], h], bits, group)
-            if of[b] >= 0:
-                k, v = torch.cat([ps[of[b]][0], k]), torch.cat([ps[of[b]][1], v])
-            w = torch.softmax(q[b, h * grp:(h + 1) * grp].double() @ k.T.contiguous() * SM, 1)
-            ref = w @ v
-            err = ((out[b, h * grp:(h + 1) * grp].double() - ref).abs().amax(1) / ref.abs().amax(1)).max()
-            worst = max(worst, float(err))
+        qs, got = (x[:, h * grp:(h + 1) * grp].double() for x in (q, out))
+        shared = {}
+        for i in set(of) - {-1}:
+            of_it = [b for b in range(batch) if of[b] == i]
+            m, l, o = _part(qs[of_it].reshape(-1, 128), *_dequantized(prefix[0][i, :, h], prefix[1][i, :, h], bits, group))
+            shared.update({b: (m[y * grp:(y + 1) * grp], l[y * grp:(y + 1) * grp], o[y * grp:(y + 1) * grp]) for y, b in enumerate(of_it)})
+        for b in range(batch):
+            parts = [_part(qs[b], *_dequantized(own[0][b, :lens[b], h], own[1][b, :lens[b], h], bits, group))] + ([shared[b]] if of[b] >= 0 else [])
+            top = torch.stack([m for m, _, _ in parts]).amax(0)
+            total = sum(l * torch.exp(m - top) for m, l, _ in parts)
+            ref = sum(o * torch.exp(m - top) for m, _, o in parts) / total
+            worst = max(worst, float(((got[b] - ref).abs().amax(1) / ref.abs().amax(1)).max()))
     assert worst <= 2e-3, worst
 
 
