@@ -524,8 +524,8 @@ int32_t tkv_prompt_attn_sizes(const tkv_prompt_desc* desc, size_t* workspace_byt
  * of q and out; rows of out, one for every head of the tokens from the first to the last of the call, must not overlap (those of q, k
  * and v may: strides of 0); sm_scale > 0 (TKV_E_INVAL otherwise).
  * Products in the inputs' type with float32 sums; softmax statistics and sums in float32, its weights rounded to the
- * inputs' type for the second product.  The result is the same bit for bit from call to call (on streams that may use as
- * many compute units).
+ * inputs' type for the second product and divided by the sum of the unrounded ones.  The result is the same bit for bit from call
+ * to call (on streams that may use as many compute units).
  * Few rows, and sequences far longer than the others, are split over the keys and joined from partial results in `workspace` (any
  * contents; 16-byte aligned; concurrent calls need separate ones).
  */

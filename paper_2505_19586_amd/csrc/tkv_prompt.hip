@@ -8,13 +8,20 @@
 // one number per lane (two lanes share a row), and its weights already lie where O^T = V^T P^T wants them: the sixteen
 // keys that a lane's weights belong to are read in that order on the V side (a sum over keys does not mind their order), by
 // LDS reads that transpose 4 x 16 elements on the way.  One pass over the keys: running maximum and
-// sum in float32, weights rounded to the inputs' type for the second product (off by at most 2^-11 or 2^-8 of each, random over
-// the keys, beside the output's own rounding of as much: against float64 2.6e-4 of the outputs' norm in fp16, 2.1e-4 of them the latter).
+// sum in float32, weights rounded to the inputs' type for the second product (off by at most 2^-11 or 2^-8 of each, beside the
+// output's own rounding of as much: against float64 2.6e-4 of the outputs' norm in fp16, 2.1e-4 of them the latter).  They are divided
+// by the sum of the unrounded ones: over keys that differ the errors differ and mostly cancel, over equal keys all weights are off
+// alike, and so is the output, by as much again as its own rounding at most.  (Divided by the sum of the rounded ones, a mixed product
+// per two of them, equal values came out exactly: 16384 tokens in fp16 2150 -> 2210 us, packed prompts in bfloat16 885 -> 920, with no
+// change of the error over keys that differ.  Not kept: the logarithm of the sum would need the other sum beside it.)
 //
-// Long prompts are bound by the LDS reads beside the matrix products (a wave reads a tile's keys and values, 32 KiB, for 32 rows; 64
-// bytes a clock and compute unit: as long as the products of both) and by the clock, which falls to 1.6-1.8 GHz under them: 32 query
-// heads over 8, causal: 4096 tokens 147 us (933 TFLOP/s), 16384 2095 us (1050; the same products alone 1553 us, without the LDS reads
-// 1770).  64 rows a wave would halve the reads but spilled 69 registers.
+// Long prompts fill no unit: the matrix cores are busy for 52 % of the time, the vector units for 44 % or more, and LDS for about 37 %
+// (a workgroup reads 128 KiB of keys, at up to 221 bytes a clock and compute unit as measured, and 128 KiB of values, transposing,
+// 150 bytes a clock, in a tile's 3950 clocks).  A turn (below) lasts 1975 clocks for 1024 of products: what bounds it is the wait of
+// products for the reads just before them and of the halves for each other, and the clock, which falls to 1.6-1.8 GHz.  32 query
+// heads over 8, causal: 4096 tokens 147-152 us (905-935 TFLOP/s), 16384 2090-2180 us (1010-1050; the same products alone 1553 us,
+// without the LDS reads 1770).  A workgroup's beginning and end, about 9 us with one of them on a unit, are hidden by nothing: a tenth
+// of 4096 tokens.  64 rows a wave would halve the reads; as the compiler placed them, 69 registers spilled.
 #include <algorithm>
 
 #include "tkv_common.h"
@@ -526,8 +533,8 @@ __global__ __launch_bounds__(64 * kFewWaves, 1) void prompt_few_kernel(PromptPar
 }
 
 // Joins the pieces of the split rows, a lane two channels.  ONE: a wave per row; otherwise a workgroup, every wave a quarter of the pieces.
-// (Whole calls with a workgroup / a wave per row: 1024 rows of 32 heads in 2 pieces 81 / 51 us, 333 rows in 12 389 / 377; one row of 32
-// heads in 32 pieces with a workgroup 9.1.)
+// (Whole calls, again and again on the same inputs, with a workgroup / a wave per row: 1024 tokens of 32 heads over 2048 keys in 2 pieces
+// 98 / 64 us, 512 over 4096 in 4 85 / 55, 333 over 65869 in 5 398 / 386; one token over 32768, in 32 pieces, 27.8 with a workgroup.)
 template <typename T, bool ONE>
 __global__ __launch_bounds__(256) void prompt_merge_kernel(PromptParams p) {
   __shared__ float acc_s[4][TKV_D], l_s[4], m_s[4];
@@ -598,8 +605,9 @@ __global__ __launch_bounds__(256) void prompt_merge_kernel(PromptParams p) {
 
 // What the plan goes by, in us: a workgroup's beginning and end and a tile of its keys (64; few rows: 32 for each wave, longer the more
 // workgroups share the memory), and the joining launch with the partial results' way out and back.  Measured with one
-// sequence, 32 query heads, 8 KV heads, whole / in pieces: 512 tokens 22 / 34, 1024 over 1024 35 / 51, 512 over 4096 107 / 56, 333 over 65869
-// 1592 / 377, one over 500 8.5 / 8.8, one over 4000 29.9 / 9.3.
+// sequence, 32 query heads, 8 KV heads, whole / in pieces: 512 tokens 22 / 34, 1024 over 1024 35 / 51, 512 over 4096 107 / 55, 333 over 65869
+// 1592 / 386, one over 500 8.5 / 8.8, one over 4000 29.9 / 9.3.  (With all units at work for long a tile takes about 2 us, as the clock falls:
+// the constants are for calls short enough that the choice matters.)
 constexpr double kFixed = 9.5, kTileTime = 1.55, kFewFixed = 5.3, kFewTile = 0.8, kFewLoad = 0.0092;
 constexpr double kJoin = 3, kJoinRow = 3e-4, kJoinPart = 1.7e-4;
 

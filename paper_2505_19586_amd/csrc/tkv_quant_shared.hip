@@ -13,13 +13,14 @@
 //     weights' own sum as the rows of one more operand.  (V-hat rounded to fp16 takes the outputs' error against float64 from 2.9e-4 of
 //     their norm to 3.5e-4, 2.1e-4 of which is their own rounding; one product instead of two at 4 bits, scaler times code rounded, to
 //     3.4e-4, for 127 us instead of 147 where 64 sequences share 32770 tokens.)  The weights are rounded to fp16, off by at most 2^-11
-//     of each, and divided by the sum of the rounded ones.
+//     of each, and divided by the sum of the rounded ones (those of tokens still in the ring added up as they are made).
 // A wave takes 32-token blocks on its own: the codes lie in the order of the 16x16x32 matrix operands, S^T = K Q^T
 // leaves a query's logits in the lanes where O^T = V^T P^T wants its weights, and nothing is exchanged
 // between lanes but a rare rise of the running maximum.
 //
-// No one unit bounds it: with 64 rows the vector units work half of the time (unpacking, exponentials) and the matrix cores a quarter (2
-// bits) to two fifths (4 bits), one wave's beside the other's of a SIMD.  131072 tokens under 16 sequences of 32/8 heads, 2 bits: 61 us (568
+// Latency bounds it: with 64 rows the vector units work half of the time or more (unpacking, exponentials) and the matrix cores a quarter
+// (2 bits) to two fifths (4 bits); a wave goes from logits over their maximum and weights to the values' products one block at a time, and
+// there are two waves on a SIMD to fill each other's gaps.  131072 tokens under 16 sequences of 32/8 heads, 2 bits: 61 us (568
 // TFLOP/s; the codes alone would take 24 us), 32770 under 64 of 64/8, 4 bits: 146 us, two prefixes of 48413, 1 bit: 23 us, 2000 under 4: 12.7 us.
 //
 // Prefix and own tokens are split over workgroups in proportion to their cost; partial (reference, sum, weighted V) results
@@ -609,7 +610,8 @@ __global__ __launch_bounds__(256) void shared_merge_kernel(SharedParams p) {
 }
 
 // What a workgroup takes, in units of 0.8 ns: a block of 32 tokens for a row group of 16 NQ, and its fixed part (a first round
-// trip, the join of its waves); measured at 2 bits.
+// trip, the join of its waves); measured at 2 bits and used for all (at 4 bits a block of 64 rows takes half as much again, which changes all
+// prefixes' parts alike).
 constexpr double block_cost(int nq) { return nq == 1 ? 200 : nq == 2 ? 300 : 464; }
 constexpr double fixed_cost(int nq) { return nq == 1 ? 6000 : nq == 2 ? 8000 : 10000; }
 constexpr int kWorkgroups = 256;  // workgroups at a time, at most: one per compute unit (it takes most of the LDS)
