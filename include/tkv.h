@@ -227,7 +227,7 @@ int32_t tkv_quant_attn_decode_shared_sizes(const tkv_quant_desc* prefix_desc, co
  * tkv_quant_attn_decode over a cache that held prefix and own tokens, quantized as they are here: the prefix's
  * newest tokens stay fp16 as its own descriptor says.
  * prefix_desc and desc: same heads, bits and group_size; residual, capacity and batch may differ.  Either may hold empty
- * sequences; a sequence without any token yields zeros.  q, out: fp16 [B][Hq][128], at multiples of 4 bytes.  sm_scale > 0.
+ * sequences; a sequence without any token yields zeros.  q, out: fp16 [B][Hq][128], at multiples of 4 bytes.  sm_scale > 0, at most 2.3e38.
  * All six settings of bits and group_size are evaluated alike: products of codes, scalers and zero-points without a rounding before
  * the float32 sums, softmax statistics in float32, its weights rounded to fp16.  Logits (sm_scale q.k) of magnitude up to 2^26 and
  * cached values of magnitude up to 30000 are safe (a dequantized value beyond 65504 is infinite).  The result is the same bit for
@@ -522,7 +522,7 @@ int32_t tkv_prompt_attn_sizes(const tkv_prompt_desc* desc, size_t* workspace_byt
  * hold).  A non-finite value in a row that a query does not see may still reach it where both lie in the same 64 keys.
  * Addresses are multiples of 16 bytes (lse: 4).  out must not overlap the inputs.  Sequences may share keys, in any order, but no row
  * of q and out; rows of out, one for every head of the tokens from the first to the last of the call, must not overlap (those of q, k
- * and v may: strides of 0); sm_scale > 0 (TKV_E_INVAL otherwise).
+ * and v may: strides of 0); 0 < sm_scale <= 2.3e38 (TKV_E_INVAL otherwise).
  * Products in the inputs' type with float32 sums; softmax statistics and sums in float32, its weights rounded to the
  * inputs' type for the second product and divided by the sum of the unrounded ones.  Logits (sm_scale q.k) of magnitude up to 2^26
  * are safe; beyond, float32 no longer tells their weights apart, and outputs can be wrong or non-finite.  The result is the same bit

@@ -675,7 +675,8 @@ extern "C" int32_t tkv_prompt_attn(const tkv_prompt_desc* d, const void* q, cons
   const int32_t st = check_prompt_desc(d);
   if (st != TKV_OK) return st;
   if (!q_start_host || !q_len_host || !k_start_host || !k_len_host || !workspace) return TKV_E_INVAL;
-  if (!(sm_scale > 0.f) || !(sm_scale <= 3.402823466e38f)) return TKV_E_INVAL;
+  const float scale2 = sm_scale * 1.4426950408889634f;
+  if (!(sm_scale > 0.f) || !(scale2 <= 3.402823466e38f)) return TKV_E_INVAL;
   if (!good_strides(d->q_stride) || !good_strides(d->k_stride) || !good_strides(d->v_stride) || !good_strides(d->o_stride)) return TKV_E_INVAL;
   PromptParams p;
   p.group = d->n_q_heads / d->n_kv_heads;
@@ -715,7 +716,7 @@ extern "C" int32_t tkv_prompt_attn(const tkv_prompt_desc* d, const void* q, cons
   p.v_st = d->v_stride[0]; p.v_sh = d->v_stride[1];
   p.o_st = d->o_stride[0]; p.o_sh = d->o_stride[1];
   p.hq = d->n_q_heads; p.hkv = d->n_kv_heads; p.batch = d->batch; p.causal = d->causal;
-  p.scale2 = sm_scale * 1.4426950408889634f;
+  p.scale2 = scale2;
 
   bool few = true;
   for (int b = 0; b < d->batch; ++b) few = few && (int64_t)q_len_host[b] * p.group <= kFew;

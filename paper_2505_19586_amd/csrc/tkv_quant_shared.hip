@@ -680,7 +680,8 @@ extern "C" int32_t tkv_quant_attn_decode_shared(const tkv_quant_desc* pd, const 
   if (st != TKV_OK) return st;
   if (!cache_ok(prefix) || !cache_ok(cache) || !q || !out || !workspace) return TKV_E_INVAL;
   if (((uintptr_t)q & 3) != 0 || ((uintptr_t)out & 3) != 0 || ((uintptr_t)workspace & 15) != 0) return TKV_E_INVAL;
-  if (!(sm_scale > 0.f) || !(sm_scale <= 3.402823466e38f)) return TKV_E_INVAL;
+  const float scale2 = sm_scale * 1.4426950408889634f;
+  if (!(sm_scale > 0.f) || !(scale2 <= 3.402823466e38f)) return TKV_E_INVAL;
   for (int i = 0; i < pd->batch; ++i)
     if (prefix->seq_len_host[i] < 0 || prefix->seq_len_host[i] > pd->capacity) return TKV_E_INVAL;
   for (int b = 0; b < d->batch; ++b) {
@@ -697,7 +698,7 @@ extern "C" int32_t tkv_quant_attn_decode_shared(const tkv_quant_desc* pd, const 
   p.out = (__half*)out;
   p.parts = (float*)workspace;
   p.ml = (float*)workspace + slots_max * TKV_D;
-  p.scale2 = sm_scale * 1.4426950408889634f;
+  p.scale2 = scale2;
   p.hq = d->n_q_heads; p.hkv = d->n_kv_heads; p.group = d->n_q_heads / d->n_kv_heads;
   p.batch = d->batch; p.n_prefix = pd->batch;
 
