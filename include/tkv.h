@@ -534,6 +534,95 @@ int32_t tkv_prompt_attn(const tkv_prompt_desc* desc, const void* q, const void* 
                         const int32_t* q_start_host, const int32_t* q_len_host, const int32_t* k_start_host,
                         const int32_t* k_len_host, float sm_scale, void* workspace, size_t workspace_bytes, void* stream);
 
+/*
+ * tkv_qk_norm_rope with positions of several axes, as of images and video (time, height, width): positions int32
+ * [n_axes][n_tokens], and frequency i turns by positions[axis_of_host[i]][token] (HOST uint8 [R/2], each below n_axes; n_axes at most 4).
+ * Any assignment goes: sections of the frequencies, axes in turn.  Everything else as there; axes that agree, or all frequencies of
+ * one axis, give the same bits.
+ */
+int32_t tkv_qk_norm_rope_axes(const tkv_rope_desc* desc, int32_t n_tokens, const void* q, const void* k, const void* v,
+                              const int32_t* positions, const float* inv_freq, const uint8_t* axis_of_host, int32_t n_axes,
+                              const void* q_weight, const void* k_weight, void* q_out, void* k_out, void* v_out, void* stream);
+
+/* ---------------------------------------------------------------------------------
+ * Paged caches: unquantized or 4-bit rows of many sequences in pages of one pool
+ * ------------------------------------------------------------------------------- */
+
+typedef struct {
+  uint32_t struct_size; /* sizeof(tkv_paged_desc)                                         */
+  int32_t n_q_heads;    /* Hq, at most 1024; a multiple of n_kv_heads, any multiple       */
+  int32_t n_kv_heads;
+  int32_t head_dim;     /* 128                                                            */
+  int32_t dtype;        /* tkv_dtype of rows, queries and outputs, and of 16-bit pages    */
+  int32_t bits;         /* 16 or 4                                                        */
+  int32_t page_size;    /* tokens of a page: 16, 32, 64, ... 1024                         */
+  int32_t n_pages;      /* n_pages * page_size < 2^31                                     */
+  int64_t k_stride[3];  /* 16 bits: strides of pages, KV heads and tokens in elements, multiples of 8, that of tokens */
+  int64_t v_stride[3];  /* at most 2^22, so that no two rows overlap; the 128 channels of a row lie side by side (4 bits: not read) */
+} tkv_paged_desc;
+
+/*
+ * A token is held at a slot: page * page_size + place within the page.  Which pages are a sequence's, in which order, says the
+ * caller's page table; everything about it lies on the device, so that a captured graph of a decode step replays over a cache that
+ * grows.
+ * 16 bits: k_pages, v_pages hold rows of 128 elements with the descriptor's strides ([n_pages][Hkv][page_size][128],
+ * [n_pages][page_size][Hkv][128], slices of one allocation).
+ * 4 bits: k_pages, v_pages are uint8 [n_pages][Hkv][68 * page_size]: the codes of all of a head's tokens, 64 bytes each (channel 2i in
+ * the low half of byte i), then the scales of all of them, 4 bytes each: byte u is the exponent + 127 of channels 32u to
+ * 32u + 31.  A code is a 4-bit floating-point number, sign, two bits of exponent, one of mantissa (0, 0.5, 1, 1.5, 2, 3, 4, 6), and stands
+ * for itself times 2^exponent; a scale of 255 stands for NaN.
+ */
+
+/* Bytes of k_pages, and of v_pages, without room between rows. */
+int32_t tkv_paged_cache_sizes(const tkv_paged_desc* desc, size_t* bytes_each);
+
+/*
+ * Keys and values of new tokens into their slots, normed and turned on the way: tkv_qk_norm_rope (axis_of_host NULL: one axis) or
+ * tkv_qk_norm_rope_axes, with rope->out_dtype = desc->dtype and the same heads, whose rows of k and v go to slots[token] (device int32
+ * [n_tokens]; below 0 or beyond the pages: the token is padding and is not held) instead of contiguous outputs.  q_out
+ * [n_tokens][Hq][128] receives the queries of every token, k_out, where not NULL, the keys as well (contiguous, in 16 bits whatever the
+ * pages; for a prompt's own attention).  q and q_out may both be NULL: keys and values alone.
+ * 4 bits: rows are rounded to desc->dtype, then every block of 32 channels gets the exponent e = floor(log2(largest magnitude)) - 2, at
+ * least -23 (TKV_F16) or -125 (TKV_BF16), and codes x / 2^e rounded to the nearest, ties to the even code, magnitudes beyond 6 to 6.
+ * What a block stands for is a number of desc->dtype.  A block that holds an infinity or NaN stands for NaN.
+ * No slot twice in one call.  Addresses of pages, rows, weights and outputs are multiples of 16 bytes.  n_tokens == 0 is a no-op.
+ */
+int32_t tkv_paged_append(const tkv_paged_desc* desc, const tkv_rope_desc* rope, int32_t n_tokens, const void* q, const void* k,
+                         const void* v, const int32_t* positions, const float* inv_freq, const uint8_t* axis_of_host, int32_t n_axes,
+                         const void* q_weight, const void* k_weight, const int32_t* slots, void* q_out, void* k_out, void* k_pages,
+                         void* v_pages, void* stream);
+
+/*
+ * Tokens read back: k_out, v_out [n_tokens][Hkv][128] of desc->dtype, contiguous, rows slots[token] (device int32; below 0 or beyond the
+ * pages: zeros; any slot any number of times): what tkv_prompt_attn takes for a chunk over a cached prefix, or the caches for
+ * tokens that move between them.
+ */
+int32_t tkv_paged_gather(const tkv_paged_desc* desc, const void* k_pages, const void* v_pages, int32_t n_tokens, const int32_t* slots,
+                         void* k_out, void* v_out, void* stream);
+
+/* Workspace bytes of tkv_paged_attn, whatever the call's sequences (any contents before a call). */
+int32_t tkv_paged_attn_sizes(const tkv_paged_desc* desc, size_t* workspace_bytes);
+
+/*
+ * Eq. 3 over pages, for decode steps, drafts of several tokens and short chunks: sequence b holds k_lens[b] tokens (device int32
+ * [batch]), token t of them at place t % page_size of page page_table[b][t / page_size] (device int32 [batch][pages_each]; entries behind
+ * the last token are not read), and its queries are its newest tokens: rows q_starts[b] to q_starts[b + 1] - 1 of q and out (device int32
+ * [batch + 1], ascending; NULL: row b alone, n_tokens = batch).  Token i of n queries sees keys j <= i + k_lens[b] - n.
+ * out = softmax(sm_scale q.k) v; a token that sees no key yields zeros, and -inf in lse.
+ * q, out [n_tokens][Hq][128] contiguous; lse float32 [n_tokens][Hq] (natural logarithm of the sum of exponentials) or NULL.  Rows of out and
+ * lse that belong to no sequence are left as they were.  max_q_len: the most queries that a sequence has, as the host knows it.
+ * Keys behind a sequence's last are never used, whatever their slots hold.  A page number outside the cache stands for rows of zeros; k_lens
+ * beyond pages_each * page_size, or below 0, count as that, or as 0.
+ * Products in desc->dtype with float32 sums (4 bits: of what the codes stand for, exactly); softmax statistics in float32.
+ * 0 < sm_scale <= 2.3e38; logits (sm_scale q.k) of magnitude up to 2^26 are safe.  The result is the same bit for bit from call to call
+ * (on streams that may use as many compute units).  Addresses of pages, q, out and workspace are multiples of 16 bytes; concurrent calls
+ * need separate workspaces.
+ */
+int32_t tkv_paged_attn(const tkv_paged_desc* desc, const void* k_pages, const void* v_pages, int32_t batch, int32_t n_tokens,
+                       int32_t max_q_len, const void* q, void* out, float* lse, const int32_t* page_table, int32_t pages_each,
+                       const int32_t* k_lens, const int32_t* q_starts, float sm_scale, void* workspace, size_t workspace_bytes,
+                       void* stream);
+
 /* ---------------------------------------------------------------------------------
  * Offline identification (Sec. 4.1): which layers are quantization-friendly
  * ------------------------------------------------------------------------------- */

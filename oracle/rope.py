@@ -8,7 +8,7 @@ import numpy as np
 
 
 def norm_rope(x, positions, inv_freq, *, norm=False, weight=None, eps=1e-6, interleaved=False):
-    """x [T, H, D] -> (rotated rows, |a| + |b| of every channel's pair before the rotation: what rounding
+    """x [T, H, D], positions [T], or [T, R/2] one for every frequency -> (rotated rows, |a| + |b| of every channel's pair before the rotation: what rounding
     errors are relative to); a row is normed over its D channels, then its first 2 len(inv_freq) channels turn."""
     x = np.asarray(x, np.float64)
     if norm:
@@ -18,7 +18,8 @@ def norm_rope(x, positions, inv_freq, *, norm=False, weight=None, eps=1e-6, inte
     y, size = x.copy(), np.abs(x)
     half = 0 if inv_freq is None else len(inv_freq)
     if half:
-        t = np.asarray(positions, np.float64)[:, None] * np.asarray(inv_freq, np.float64)[None, :]
+        at = np.asarray(positions, np.float64)
+        t = (at[:, None] if at.ndim == 1 else at) * np.asarray(inv_freq, np.float64)[None, :]
         for i in range(half):
             a, b = (2 * i, 2 * i + 1) if interleaved else (i, i + half)
             c, s = np.cos(t[:, i])[:, None], np.sin(t[:, i])[:, None]

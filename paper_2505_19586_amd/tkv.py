@@ -76,6 +76,12 @@ class PromptDesc(C.Structure):
                 ("reserved", C.c_int32), ("strides", C.c_int64 * 8)]  # of tokens and heads: q, k, v, out
 
 
+class PagedDesc(C.Structure):
+    _fields_ = [("struct_size", C.c_uint32), ("n_q_heads", C.c_int32), ("n_kv_heads", C.c_int32),
+                ("head_dim", C.c_int32), ("dtype", C.c_int32), ("bits", C.c_int32), ("page_size", C.c_int32),
+                ("n_pages", C.c_int32), ("k_stride", C.c_int64 * 3), ("v_stride", C.c_int64 * 3)]  # of pages, heads, tokens
+
+
 def lib() -> C.CDLL:
     """Loads libtkv.so (built by paper_2505_19586_amd/build.py); raises if absent."""
     global _LIB
@@ -125,6 +131,12 @@ def lib() -> C.CDLL:
         L.tkv_dense_preference.argtypes = [C.POINTER(PrefDesc), vp, vp, i32, C.c_float, vp, vp, sz, vp]
         L.tkv_classify_layer.argtypes = [C.POINTER(C.c_float), i32, i32, C.c_float, C.POINTER(C.c_float)]
         L.tkv_qk_norm_rope.argtypes = [C.POINTER(RopeDesc), i32] + [vp] * 11
+        L.tkv_qk_norm_rope_axes.argtypes = [C.POINTER(RopeDesc), i32] + [vp] * 6 + [i32] + [vp] * 6
+        L.tkv_paged_cache_sizes.argtypes = [C.POINTER(PagedDesc), C.POINTER(sz)]
+        L.tkv_paged_append.argtypes = [C.POINTER(PagedDesc), C.POINTER(RopeDesc), i32] + [vp] * 6 + [i32] + [vp] * 8
+        L.tkv_paged_gather.argtypes = [C.POINTER(PagedDesc), vp, vp, i32] + [vp] * 4
+        L.tkv_paged_attn_sizes.argtypes = [C.POINTER(PagedDesc), C.POINTER(sz)]
+        L.tkv_paged_attn.argtypes = [C.POINTER(PagedDesc), vp, vp, i32, i32, i32, vp, vp, vp, vp, i32, vp, vp, C.c_float, vp, sz, vp]
         L.tkv_prompt_attn_sizes.argtypes = [C.POINTER(PromptDesc), C.POINTER(sz)]
         L.tkv_prompt_attn.argtypes = [C.POINTER(PromptDesc)] + [vp] * 9 + [C.c_float, vp, sz, vp]
         L.tkv_quant_attn_decode_shared_sizes.argtypes = [C.POINTER(QuantDesc), C.POINTER(QuantDesc), C.POINTER(sz)]
@@ -143,7 +155,8 @@ def lib() -> C.CDLL:
                      "tkv_sparse_prefetch_keys", "tkv_sparse_estimate_topk_cm",
                      "tkv_sparse_select_estimate_topk", "tkv_sparse_append_dynamic",
                      "tkv_sparse_append_estimate_topk", "tkv_sparse_decode", "tkv_dense_preference_sizes", "tkv_dense_preference",
-                     "tkv_classify_layer", "tkv_qk_norm_rope",
+                     "tkv_classify_layer", "tkv_qk_norm_rope", "tkv_qk_norm_rope_axes", "tkv_paged_cache_sizes",
+                     "tkv_paged_append", "tkv_paged_gather", "tkv_paged_attn_sizes", "tkv_paged_attn",
                      "tkv_prompt_attn_sizes", "tkv_prompt_attn", "tkv_quant_attn_decode_shared_sizes",
                      "tkv_quant_attn_decode_shared"):
             getattr(L, name).restype = C.c_int32
@@ -194,11 +207,12 @@ class _Workspaces:
     other and beside eager calls.  Threads hold `lock` while their call's launches go out, so that none of another thread's, with
     the same workspace, comes in between."""
 
-    def __init__(self, n_bytes: int, device: torch.device):
+    def __init__(self, n_bytes: int, device: torch.device, at_once: bool = True):
         self._bytes, self._device, self._of = n_bytes, device, {}
         self.lock = threading.Lock()
-        with torch.cuda.device(device):
-            self.of(_stream(None))
+        if at_once:
+            with torch.cuda.device(device):
+                self.of(_stream(None))
 
     def of(self, handle: int, stream=None) -> torch.Tensor:
         captured = torch._C._cuda_isCurrentStreamCapturing()
@@ -625,50 +639,212 @@ class Stage1:
 _DTYPES = {torch.float16: 0, torch.bfloat16: 1}
 
 
-def qk_norm_rope(q: torch.Tensor, k: torch.Tensor, positions: torch.Tensor | None, inv_freq: torch.Tensor | None, *,
-                 v: torch.Tensor | None = None, norm: bool = False, q_weight: torch.Tensor | None = None,
-                 k_weight: torch.Tensor | None = None, eps: float = 1e-6, interleaved: bool = False,
-                 out_dtype: torch.dtype | None = None, q_out: torch.Tensor | None = None,
-                 k_out: torch.Tensor | None = None, v_out: torch.Tensor | None = None, stream=None):
-    """tkv_qk_norm_rope: q [T, Hq, 128], k, v [T, Hkv, 128] (fp16 or bf16, views of one fused projection
-    allowed), positions int32 [T], inv_freq float32 [R/2] (None: no rotation) -> contiguous (q_out, k_out, v_out or
-    None) in out_dtype (default: the inputs')."""
-    t, hq, ch = shape_q = q.shape
-    t2, hkv, ch2 = shape_k = k.shape
-    dt, dev, at = q.dtype, q.device, q.get_device()  # (numbers of devices compare in a third of the time of devices)
-    assert q.is_cuda and t2 == t and ch2 == ch and k.dtype == dt and k.get_device() == at
-    _on_current(q, stream)
-    sq, sk, sv = q.stride(), k.stride(), (0, 0, 1)
+def rope_axes(sections, interleaved: bool = False) -> bytes:
+    """The axis of each frequency, for `axis_of`: sections[a] of them belong to axis a, one section after the other, or
+    (interleaved) the axes in turn while they have any left."""
+    left = [int(n) for n in sections]
+    if not interleaved:
+        return bytes(a for a, n in enumerate(left) for _ in range(n))
+    out = []
+    while any(left):
+        for a, n in enumerate(left):
+            if n:
+                out.append(a)
+                left[a] -= 1
+    return bytes(out)
+
+
+def _rotation(q, k, positions, inv_freq, axis_of, norm, q_weight, k_weight, eps, interleaved, v, out_dtype, n_q_heads=None):
+    """What qk_norm_rope and PagedCache.append check and describe alike (q None: its heads count as n_q_heads):
+    the descriptor and n_axes."""
+    shape_k = k.shape
+    t, hkv, ch = shape_k
+    dt, at = k.dtype, k.get_device()  # (numbers of devices compare in a third of the time of devices)
+    assert k.is_cuda
+    sq, sk, sv = (0, 0, 1), k.stride(), (0, 0, 1)
+    if q is not None:
+        tq, n_q_heads, chq = q.shape
+        assert tq == t and chq == ch and q.dtype == dt and q.get_device() == at
+        sq = q.stride()
     if v is not None:
         assert v.shape == shape_k and v.dtype == dt and v.get_device() == at
         sv = v.stride()
     assert sq[2] == 1 and sk[2] == 1 and sv[2] == 1
-    rot = 0
+    rot, n_axes = 0, 1
     if inv_freq is not None:
         assert inv_freq.dtype == torch.float32 and inv_freq.dim() == 1 and inv_freq.is_contiguous() and inv_freq.get_device() == at
         assert positions is not None and positions.dtype == torch.int32 and positions.get_device() == at
-        assert positions.shape == (t,) and positions.is_contiguous()
+        assert positions.is_contiguous()
         rot = 2 * inv_freq.shape[0]
+        if axis_of is None:
+            assert positions.shape == (t,)
+        else:
+            n_axes, tp = positions.shape
+            assert tp == t and 2 * len(axis_of) == rot, "axis_of: an axis for every frequency"
     for w in (q_weight, k_weight):
         assert w is None or (w.shape == (ch,) and w.is_contiguous() and w.dtype == dt and w.get_device() == at)
+    # (an axis of one element: torch leaves its stride to chance)
+    by_t, by_q, by_k = t > 1, n_q_heads > 1, hkv > 1
+    return RopeDesc(C.sizeof(RopeDesc), n_q_heads, hkv, ch, _DTYPES.get(dt, -1), _DTYPES.get(out_dtype, -1), norm, eps, rot, interleaved,
+                    by_t * sq[0], by_q * sq[1], by_t * sk[0], by_k * sk[1], by_t * sv[0], by_k * sv[1]), n_axes
+
+
+def qk_norm_rope(q: torch.Tensor, k: torch.Tensor, positions: torch.Tensor | None, inv_freq: torch.Tensor | None, *,
+                 v: torch.Tensor | None = None, norm: bool = False, q_weight: torch.Tensor | None = None,
+                 k_weight: torch.Tensor | None = None, eps: float = 1e-6, interleaved: bool = False, axis_of=None,
+                 out_dtype: torch.dtype | None = None, q_out: torch.Tensor | None = None,
+                 k_out: torch.Tensor | None = None, v_out: torch.Tensor | None = None, stream=None):
+    """tkv_qk_norm_rope: q [T, Hq, 128], k, v [T, Hkv, 128] (fp16 or bf16, views of one fused projection
+    allowed), positions int32 [T], inv_freq float32 [R/2] (None: no rotation) -> contiguous (q_out, k_out, v_out or
+    None) in out_dtype (default: the inputs').  With axis_of (bytes or small numbers, an axis for every frequency; see rope_axes) positions
+    are int32 [axes, T]: tkv_qk_norm_rope_axes."""
+    shape_q, shape_k = q.shape, k.shape
+    dt, dev, at = q.dtype, q.device, q.get_device()
+    _on_current(q, stream)
+    if axis_of is not None:
+        axis_of = bytes(axis_of)
     if out_dtype is None:
         out_dtype = next((x.dtype for x in (q_out, k_out, v_out) if x is not None), dt)
+    desc, n_axes = _rotation(q, k, positions, inv_freq, axis_of, norm, q_weight, k_weight, eps, interleaved, v, out_dtype)
     for o, shape in ((q_out, shape_q), (k_out, shape_k), (v_out, shape_k if v is not None else None)):
         assert o is None or (o.dtype == out_dtype and o.shape == shape and o.is_contiguous() and o.get_device() == at)
     if q_out is None:
-        q_out = _new((t, hq, ch), out_dtype, dev, stream)
+        q_out = _new(shape_q, out_dtype, dev, stream)
     if k_out is None:
-        k_out = _new((t, hkv, ch), out_dtype, dev, stream)
+        k_out = _new(shape_k, out_dtype, dev, stream)
     if v_out is None and v is not None:
-        v_out = _new((t, hkv, ch), out_dtype, dev, stream)
-    # (an axis of one element: torch leaves its stride to chance)
-    by_t, by_q, by_k = t > 1, hq > 1, hkv > 1
-    desc = RopeDesc(C.sizeof(RopeDesc), hq, hkv, ch, _DTYPES.get(dt, -1), _DTYPES.get(out_dtype, -1), norm, eps, rot, interleaved,
-                    by_t * sq[0], by_q * sq[1], by_t * sk[0], by_k * sk[1], by_t * sv[0], by_k * sv[1])
-    _check(lib().tkv_qk_norm_rope(C.byref(desc), t, q.data_ptr(), k.data_ptr(), _ptr(v), _ptr(positions) if rot else 0,
-                                  _ptr(inv_freq) if rot else 0, _ptr(q_weight), _ptr(k_weight), q_out.data_ptr(), k_out.data_ptr(),
-                                  _ptr(v_out), _stream(stream)), "tkv_qk_norm_rope")
+        v_out = _new(shape_k, out_dtype, dev, stream)
+    pos, freq = (_ptr(positions), _ptr(inv_freq)) if desc.rotary_dim else (0, 0)
+    outs = q_out.data_ptr(), k_out.data_ptr(), _ptr(v_out), _stream(stream)
+    if axis_of is None:
+        _check(lib().tkv_qk_norm_rope(C.byref(desc), shape_q[0], q.data_ptr(), k.data_ptr(), _ptr(v), pos, freq, _ptr(q_weight),
+                                      _ptr(k_weight), *outs), "tkv_qk_norm_rope")
+    else:
+        _check(lib().tkv_qk_norm_rope_axes(C.byref(desc), shape_q[0], q.data_ptr(), k.data_ptr(), _ptr(v), pos, freq, axis_of, n_axes,
+                                           _ptr(q_weight), _ptr(k_weight), *outs), "tkv_qk_norm_rope_axes")
     return q_out, k_out, v_out
+
+
+class PagedCache:
+    """A pool of pages that hold keys and values of many sequences, in 16 bits or as microscaled 4-bit floating-point numbers
+    (tkv_paged_append, tkv_paged_gather, tkv_paged_attn).  Which pages are whose is the caller's: token t of a sequence whose pages are
+    `row` is at slot row[t // page_size] * page_size + t % page_size.  Slots, tables and lengths are device tensors, so a captured decode
+    step replays over a cache that grows.  Streams, threads and captured graphs may use one object at the same time (each stream and graph
+    has a workspace of its own); calls that write slots and calls that read them are the caller's to order.
+
+    k_pages, v_pages: the pages, where they are the caller's: [n_pages, Hkv, page_size, 128] of dtype (views with any strides whose rows do
+    not overlap), or with 4 bits uint8 [n_pages, Hkv, 68 * page_size]; made here (zeros) from n_pages otherwise."""
+
+    def __init__(self, *, n_q_heads=32, n_kv_heads=8, head_dim=128, dtype=torch.float16, bits=16, page_size=64, n_pages=None,
+                 k_pages: torch.Tensor | None = None, v_pages: torch.Tensor | None = None, device="cuda:0"):
+        assert (k_pages is None) == (v_pages is None)
+        if k_pages is None:
+            dev = _require_gpu(device)
+            row = (page_size, head_dim) if bits == 16 else (68 * page_size,)
+            k_pages, v_pages = (torch.zeros(n_pages, n_kv_heads, *row, dtype=dtype if bits == 16 else torch.uint8, device=dev)
+                                for _ in range(2))
+        assert n_pages is None or n_pages == k_pages.shape[0]
+        strides = []
+        for x in (k_pages, v_pages):
+            assert x.is_cuda and x.get_device() == k_pages.get_device()
+            if bits == 16:
+                assert x.dtype == dtype and tuple(x.shape) == (k_pages.shape[0], n_kv_heads, page_size, head_dim) and x.stride(3) == 1
+                strides.append((C.c_int64 * 3)(*(x.stride(i) if x.shape[i] > 1 else 0 for i in range(3))))
+            else:
+                assert x.dtype == torch.uint8 and tuple(x.shape) == (k_pages.shape[0], n_kv_heads, 68 * page_size) and x.is_contiguous()
+                strides.append((C.c_int64 * 3)())
+        self.desc = PagedDesc(C.sizeof(PagedDesc), n_q_heads, n_kv_heads, head_dim, _DTYPES.get(dtype, -1), bits, page_size,
+                              k_pages.shape[0], *strides)
+        ws = C.c_size_t()
+        _check(lib().tkv_paged_attn_sizes(C.byref(self.desc), C.byref(ws)), "tkv_paged_attn_sizes")
+        self.workspace_bytes = int(ws.value)
+        self.k_pages, self.v_pages, self.dtype = k_pages, v_pages, dtype
+        self.device, self._at = k_pages.device, k_pages.get_device()
+        self._pages = k_pages.data_ptr(), v_pages.data_ptr()
+        self._rows = (n_q_heads, head_dim), (n_kv_heads, head_dim)
+        self._workspaces = _Workspaces(self.workspace_bytes, torch.device("cuda", self._at), at_once=False)  # (a cache that is only filled needs none)
+
+    def _slots(self, slots, t):
+        assert slots.dtype == torch.int32 and slots.shape == (t,) and slots.is_contiguous() and slots.get_device() == self._at
+
+    def append(self, q: torch.Tensor | None, k: torch.Tensor, v: torch.Tensor, slots: torch.Tensor,
+               positions: torch.Tensor | None = None, inv_freq: torch.Tensor | None = None, *, axis_of=None, norm: bool = False,
+               q_weight: torch.Tensor | None = None, k_weight: torch.Tensor | None = None, eps: float = 1e-6, interleaved: bool = False,
+               q_out: torch.Tensor | None = None, k_out: torch.Tensor | None = None, stream=None):
+        """tkv_paged_append: q [T, Hq, 128], k, v [T, Hkv, 128] and the rotation as for qk_norm_rope; k and v go to slots (int32 [T],
+        below 0: nowhere).  Returns q_out [T, Hq, 128] (None without q); k_out [T, Hkv, 128], where given, receives the turned keys
+        too."""
+        t, at = k.shape[0], self._at
+        assert k.get_device() == at and v is not None and k.shape[1:] == self._rows[1] and (q is None or q.shape[1:] == self._rows[0])
+        _on_current(k, stream)
+        self._slots(slots, t)
+        if axis_of is not None:
+            axis_of = bytes(axis_of)
+        desc, n_axes = _rotation(q, k, positions, inv_freq, axis_of, norm, q_weight, k_weight, eps, interleaved, v, self.dtype,
+                                 self.desc.n_q_heads)
+        if q is None:
+            assert q_out is None
+        elif q_out is None:
+            q_out = _new(q.shape, self.dtype, q.device, stream)
+        for o, x in ((q_out, q), (k_out, k)):
+            assert o is None or (o.dtype == self.dtype and o.shape == x.shape and o.is_contiguous() and o.get_device() == at)
+        pos, freq = (_ptr(positions), _ptr(inv_freq)) if desc.rotary_dim else (0, 0)
+        _check(lib().tkv_paged_append(C.byref(self.desc), C.byref(desc), t, _ptr(q), k.data_ptr(), v.data_ptr(), pos, freq, axis_of,
+                                      n_axes, _ptr(q_weight), _ptr(k_weight), slots.data_ptr(), _ptr(q_out), _ptr(k_out),
+                                      *self._pages, _stream(stream)), "tkv_paged_append")
+        return q_out
+
+    def gather(self, slots: torch.Tensor, k_out: torch.Tensor | None = None, v_out: torch.Tensor | None = None, stream=None):
+        """tkv_paged_gather: the tokens at slots (int32 [T], below 0: zeros) as contiguous k, v [T, Hkv, 128]."""
+        t = slots.shape[0]
+        self._slots(slots, t)
+        _on_current(slots, stream)
+        outs = []
+        for o in (k_out, v_out):
+            if o is None:
+                o = _new((t, *self._rows[1]), self.dtype, self.device, stream)
+            else:
+                assert o.dtype == self.dtype and o.shape == (t, *self._rows[1]) and o.is_contiguous() and o.get_device() == self._at
+            outs.append(o)
+        _check(lib().tkv_paged_gather(C.byref(self.desc), *self._pages, t, slots.data_ptr(), outs[0].data_ptr(), outs[1].data_ptr(),
+                                      _stream(stream)), "tkv_paged_gather")
+        return outs[0], outs[1]
+
+    def attend(self, q: torch.Tensor, sm_scale: float, page_table: torch.Tensor, k_lens: torch.Tensor, *,
+               q_starts: torch.Tensor | None = None, max_q_len: int = 1, out: torch.Tensor | None = None,
+               lse: bool | torch.Tensor = False, stream=None):
+        """tkv_paged_attn: q [T, Hq, 128]; page_table int32 [B, pages], k_lens int32 [B]: each sequence's pages and tokens, the queries'
+        own among them; q_starts int32 [B + 1]: where each sequence's rows of q begin, max_q_len of them at most (None: row b is
+        sequence b's only one).  Returns out [T, Hq, 128], or (out, lse [T, Hq]) where lse is True or a float32 tensor.  Rows of no
+        sequence are left as they were (a new out has zeros there)."""
+        t, at, d = q.shape[0], self._at, self.desc
+        b, each = page_table.shape
+        assert q.dtype == self.dtype and q.shape[1:] == self._rows[0] and q.is_contiguous() and q.get_device() == at
+        _on_current(q, stream)
+        assert page_table.dtype == torch.int32 and page_table.is_contiguous() and page_table.get_device() == at
+        assert k_lens.dtype == torch.int32 and k_lens.shape == (b,) and k_lens.is_contiguous() and k_lens.get_device() == at
+        if q_starts is None:
+            assert t == b
+        else:
+            assert q_starts.dtype == torch.int32 and q_starts.shape == (b + 1,) and q_starts.is_contiguous() and q_starts.get_device() == at
+        if out is None:
+            out = _new(q.shape, q.dtype, q.device, stream, None if q_starts is None else 0.0)
+        else:
+            assert out.dtype == q.dtype and out.shape == q.shape and out.is_contiguous() and out.get_device() == at
+        if lse is True:
+            lse = _new((t, d.n_q_heads), torch.float32, q.device, stream, None if q_starts is None else -float("inf"))
+        elif lse is False or lse is None:
+            lse = None
+        else:
+            assert lse.dtype == torch.float32 and lse.shape == q.shape[:2] and lse.is_contiguous() and lse.get_device() == at
+        handle = _stream(stream)
+        with self._workspaces.lock:
+            workspace = self._workspaces.of(handle, stream)
+            status = lib().tkv_paged_attn(C.byref(d), *self._pages, b, t, int(max_q_len), q.data_ptr(), out.data_ptr(), _ptr(lse),
+                                          page_table.data_ptr(), each, k_lens.data_ptr(), _ptr(q_starts), float(sm_scale),
+                                          workspace.data_ptr(), self.workspace_bytes, handle)
+        _check(status, "tkv_paged_attn")
+        return out if lse is None else (out, lse)
 
 
 class PromptAttention:

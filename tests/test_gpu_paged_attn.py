@@ -1,0 +1,338 @@
+"""tkv_paged_attn against float64: lengths from none to many tiles, page sizes, head groups, types, drafts and chunks, what lies behind
+a sequence's tokens, pages that are shared or outside, streams and replayed graphs.
+
+Tolerance: with u = half a step of the type (fp16 2^-11, bf16 2^-8), a weight is rounded once (u, relative), the output once
+(u, relative), the sums and logits are float32 (products of 16-bit numbers are exact there, and 4-bit codes stand for such): |o - ref| <=
+u |ref| + 1.1 u sum_j w_j |v_j|, w the exact weights.  The logarithm of the sum: 1e-5 absolute (float32 logits of magnitude up to 32:
+128 terms, 2^-24 each)."""
+import numpy as np
+import pytest
+import torch
+
+import paper_2505_19586_amd as tkv
+from oracle import paged
+from oracle.prompt import prompt_attention
+
+pytestmark = pytest.mark.gpu
+SM = 128 ** -0.5
+HALF_STEP = {torch.float16: 2.0 ** -11, torch.bfloat16: 2.0 ** -8}
+
+
+def _f64(x):
+    return x.double().cpu().numpy()
+
+
+def _compare(out, lse, q, k, v, dtype, sm=SM):
+    ref, ref_lse = prompt_attention(q, k, v, sm)
+    size, _ = prompt_attention(q, k, np.abs(v), sm)
+    u = HALF_STEP[dtype]
+    tiny = 2.0 ** -25 if dtype == torch.float16 else 0.0
+    err = np.abs(_f64(out) - ref)
+    assert (err <= u * np.abs(ref) + 1.1 * u * size + tiny).all(), float((err / (u * size + 1e-30)).max())
+    lse = _f64(lse)
+    assert np.array_equal(np.isneginf(lse), np.isneginf(ref_lse))
+    seen = np.isfinite(ref_lse)
+    assert np.abs(lse[seen] - ref_lse[seen]).max(initial=0.0) <= 1e-5
+
+
+def _filled(k_lens, hkv, page, bits, dtype, seed=0, spare=3):
+    """A cache whose sequences' tokens lie in pages in any order, NaN in every slot behind them: cache, table, k, v (float64, by sequence)."""
+    g = torch.Generator(device="cuda").manual_seed(seed)
+    used = [-(-n // page) for n in k_lens]
+    n_pages = sum(used) + spare
+    order = torch.randperm(n_pages, generator=torch.Generator().manual_seed(seed)).tolist()
+    each = max(max(used), 1)
+    table = torch.full((len(k_lens), each), 2**31 - 1, dtype=torch.int32)    # (never looked at behind the last page)
+    nan = float("nan")
+    if bits == 16:
+        pages = [torch.full((n_pages, hkv, page, 128), nan, device="cuda").to(dtype) for _ in range(2)]
+    else:
+        pages = [torch.full((n_pages, hkv, 68 * page), 255, device="cuda", dtype=torch.uint8) for _ in range(2)]
+    cache = tkv.PagedCache(n_q_heads=hkv, n_kv_heads=hkv, page_size=page, bits=bits, dtype=dtype, k_pages=pages[0], v_pages=pages[1])
+    rows, at = [], 0
+    for b, n in enumerate(k_lens):
+        table[b, :used[b]] = torch.tensor(order[at:at + used[b]], dtype=torch.int32)
+        at += used[b]
+        k, v = ((torch.randn(n, hkv, 128, generator=g, device="cuda") * gain).to(dtype) for gain in (1.0, 1.0))
+        slots = torch.from_numpy(paged.sequence_slots(table[b].numpy(), n, page).astype(np.int32)).cuda()
+        cache.append(None, k, v, slots)
+        if bits == 4:
+            k, v = cache.gather(slots)
+        rows.append((_f64(k), _f64(v)))
+    return pages, table.cuda(), rows
+
+
+def _run(q_lens, k_lens, hq, hkv, page=64, bits=16, dtype=torch.float16, seed=0, starts=True, most=None):
+    pages, table, rows = _filled(k_lens, hkv, page, bits, dtype, seed)
+    cache = tkv.PagedCache(n_q_heads=hq, n_kv_heads=hkv, page_size=page, bits=bits, dtype=dtype, k_pages=pages[0], v_pages=pages[1])
+    g = torch.Generator(device="cuda").manual_seed(seed + 100)
+    q = torch.randn(sum(q_lens), hq, 128, generator=g, device="cuda").to(dtype)
+    lens = torch.tensor(k_lens, device="cuda", dtype=torch.int32)
+    at = torch.tensor([0, *np.cumsum(q_lens)], device="cuda", dtype=torch.int32) if starts else None
+    out, lse = cache.attend(q, SM, table, lens, q_starts=at, max_q_len=most or max(max(q_lens), 1), lse=True)
+    torch.cuda.synchronize()
+    x = _f64(q)
+    q0 = 0
+    for nq, (k, v) in zip(q_lens, rows):
+        _compare(out[q0:q0 + nq], lse[q0:q0 + nq], x[q0:q0 + nq], k, v, dtype)
+        q0 += nq
+    again, lse2 = cache.attend(q, SM, table, lens, q_starts=at, max_q_len=most or max(max(q_lens), 1), lse=True)
+    assert torch.equal(out, again) and torch.equal(lse, lse2)
+    return cache, q, table, lens, out
+
+
+BOTH = pytest.mark.parametrize("bits", [16, 4])
+
+
+@BOTH
+@pytest.mark.parametrize("dtype", [torch.float16, torch.bfloat16])
+@pytest.mark.parametrize("n", [1, 2, 15, 16, 17, 31, 32, 33, 63, 64, 65, 127, 128, 129, 500, 1030])
+def test_single_tokens(n, dtype, bits):
+    print(f"case single token over {n} {dtype} {bits} bits", flush=True)
+    _run([1], [n], 8, 2, 16 if n % 2 else 64, bits, dtype, seed=n, starts=False)
+
+
+@BOTH
+@pytest.mark.parametrize("page", [16, 32, 64, 128, 1024])
+def test_page_sizes_and_lengths_of_a_batch(page, bits):
+    print(f"case page {page} {bits} bits", flush=True)
+    _run([1] * 9, [700, 1, 0, 33, 1025, 64, 300, 128, 15], 8, 2, page, bits, seed=page, starts=False)
+
+
+@BOTH
+@pytest.mark.parametrize("hq,hkv", [(1, 1), (3, 1), (5, 5), (14, 2), (16, 1), (17, 1), (33, 1), (64, 1), (80, 1), (32, 4)])
+def test_head_groups(hq, hkv, bits):
+    print(f"case heads {hq}/{hkv} {bits} bits", flush=True)
+    _run([1, 1], [150, 333], hq, hkv, 32, bits, seed=hq, starts=False)
+    _run([2, 5], [90, 170], hq, hkv, 32, bits, seed=hq)
+
+
+@BOTH
+@pytest.mark.parametrize("dtype", [torch.float16, torch.bfloat16])
+def test_drafts_chunks_and_empty_sequences(dtype, bits):
+    print(f"case drafts {dtype} {bits} bits", flush=True)
+    _run([1, 0, 5, 3, 64, 1, 8, 2], [1, 70, 130, 300, 64, 515, 0, 1], 8, 2, 16, bits, dtype, seed=3)
+
+
+@BOTH
+@pytest.mark.parametrize("nq,nk", [(100, 37), (100, 100), (150, 700), (1, 3000), (7, 2111)])
+def test_chunks_longer_than_a_tile_of_rows(nq, nk, bits):
+    print(f"case chunk {nq} over {nk} {bits} bits", flush=True)
+    _run([nq], [nk], 8, 2, 64, bits, seed=nk)
+
+
+@BOTH
+def test_many_sequences(bits):
+    """More than a wave has lanes, and more than a workgroup has threads."""
+    print(f"case many sequences {bits} bits", flush=True)
+    lens = [(37 * b) % 90 for b in range(130)]
+    _run([1] * 130, lens, 4, 1, 16, bits, seed=1, starts=False)
+    _run([b % 3 for b in range(300)], [(b * 7) % 40 for b in range(300)], 2, 1, 16, bits, seed=2)
+
+
+@BOTH
+def test_one_long_sequence_among_short_ones(bits):
+    print(f"case ragged {bits} bits", flush=True)
+    _run([1] * 20, [20011] + [5 + b for b in range(19)], 8, 2, 64, bits, seed=4, starts=False)
+
+
+@BOTH
+def test_long_single_sequence(bits):
+    print(f"case long {bits} bits", flush=True)
+    _run([1], [33333], 4, 1, 64, bits, seed=5, starts=False)
+    _run([3], [9000], 8, 2, 64, bits, torch.bfloat16, seed=6)
+
+
+def test_a_bound_on_queries_that_is_not_reached_or_too_small():
+    """max_q_len is what the host knows: the result is right whatever it says."""
+    for most in (1, 2, 9, 1000):
+        _run([3, 1, 40], [50, 77, 130], 8, 2, 32, 16, seed=7, most=most)
+
+
+def test_rows_of_no_sequence_are_left():
+    cache, q, table, lens, want = _run([2, 3], [40, 50], 4, 2, 16, 16, seed=8)
+    wide = torch.randn(9, 4, 128, device="cuda").half()
+    wide[2:7] = q
+    starts = torch.tensor([2, 4, 7], device="cuda", dtype=torch.int32)
+    out, lse = torch.full_like(wide, 7.0), torch.full((9, 4), 5.0, device="cuda")
+    got = cache.attend(wide, SM, table, lens, q_starts=starts, max_q_len=3, out=out, lse=lse)
+    torch.cuda.synchronize()
+    assert got[0] is out and torch.equal(out[2:7], want)
+    assert (out[:2] == 7).all() and (out[7:] == 7).all() and (lse[:2] == 5).all() and (lse[7:] == 5).all() and lse[2:7].isfinite().all()
+    new = cache.attend(wide, SM, table, lens, q_starts=starts, max_q_len=3)
+    assert torch.equal(new[2:7], want) and not new[:2].any() and not new[7:].any()
+
+
+@BOTH
+def test_lengths_beyond_the_table_and_below_zero(bits):
+    page = 32
+    cache, q, table, lens, _ = _run([1, 1], [64, 96], 4, 1, page, bits, seed=9, starts=False)
+    bad = torch.tensor([-5, 2**31 - 1], device="cuda", dtype=torch.int32)
+    out, lse = cache.attend(q, SM, table, bad, lse=True)
+    want = cache.attend(q, SM, table, lens)
+    torch.cuda.synchronize()
+    assert not out[0].any() and torch.isneginf(lse[0]).all()
+    assert torch.equal(out[1], want[1])
+
+
+@BOTH
+def test_pages_outside_the_cache_stand_for_zeros(bits):
+    page = 16
+    pages, table, rows = _filled([80], 1, page, bits, torch.float16, seed=10)
+    cache = tkv.PagedCache(n_q_heads=4, n_kv_heads=1, page_size=page, bits=bits, k_pages=pages[0], v_pages=pages[1])
+    q = torch.randn(1, 4, 128, device="cuda").half()
+    k, v = (x.copy() for x in rows[0])
+    for place, bad in ((1, -1), (3, pages[0].shape[0])):
+        table[0, place] = bad
+        k[place * page:(place + 1) * page] = 0
+        v[place * page:(place + 1) * page] = 0
+    out, lse = cache.attend(q, SM, table, torch.tensor([80], device="cuda", dtype=torch.int32), lse=True)
+    torch.cuda.synchronize()
+    _compare(out, lse, _f64(q), k, v, torch.float16)
+
+
+@BOTH
+def test_shared_pages(bits):
+    """Sequences whose first pages are the same ones."""
+    page = 16
+    pages, table, rows = _filled([64, 40], 2, page, bits, torch.float16, seed=11)
+    cache = tkv.PagedCache(n_q_heads=4, n_kv_heads=2, page_size=page, bits=bits, k_pages=pages[0], v_pages=pages[1])
+    both = torch.cat((table, table[:1]))
+    both[2, 2] = table[1, 0]                          # 32 tokens of the first, then 16 of the second
+    q = torch.randn(3, 4, 128, device="cuda").half()
+    out, lse = cache.attend(q, SM, both, torch.tensor([64, 40, 47], device="cuda", dtype=torch.int32), lse=True)
+    torch.cuda.synchronize()
+    k, v = (np.concatenate((rows[0][i][:32], rows[1][i][:15])) for i in range(2))
+    for b, (kk, vv) in enumerate((rows[0], rows[1], (k, v))):
+        _compare(out[b:b + 1], lse[b:b + 1], _f64(q[b:b + 1]), kk, vv, torch.float16)
+
+
+@pytest.mark.parametrize("layout", ["tokens first", "both in one"])
+def test_strides_of_pages(layout):
+    hq, hkv, page, n_pages, dt = 8, 2, 32, 7, torch.float16
+    if layout == "tokens first":
+        k, v = (torch.randn(n_pages, page, hkv, 128, device="cuda").to(dt).transpose(1, 2) for _ in range(2))
+    else:
+        both = torch.randn(n_pages, 2, hkv, page, 128, device="cuda").to(dt)
+        k, v = both[:, 0], both[:, 1]
+    cache = tkv.PagedCache(n_q_heads=hq, n_kv_heads=hkv, page_size=page, k_pages=k, v_pages=v)
+    table = torch.tensor([[5, 1, 0, 6]], device="cuda", dtype=torch.int32)
+    q = torch.randn(1, hq, 128, device="cuda").to(dt)
+    out, lse = cache.attend(q, SM, table, torch.tensor([123], device="cuda", dtype=torch.int32), lse=True)
+    torch.cuda.synchronize()
+    kk, vv = (_f64(x)[[5, 1, 0, 6]].transpose(0, 2, 1, 3).reshape(-1, hkv, 128)[:123] for x in (k, v))
+    _compare(out, lse, _f64(q), kk, vv, dt)
+
+
+@BOTH
+def test_far_logits_and_large_values(bits):
+    """Logits of thousands (one weight is all), and values near the type's largest."""
+    page, dt = 32, torch.float16
+    k = (60 * torch.randn(200, 1, 128, device="cuda")).to(dt)
+    v = (20000 * torch.randn(200, 1, 128, device="cuda")).clamp(-60000, 60000).to(dt)
+    cache = tkv.PagedCache(n_q_heads=4, n_kv_heads=1, page_size=page, bits=bits, n_pages=7)
+    slots = torch.arange(200, device="cuda", dtype=torch.int32)
+    cache.append(None, k, v, slots)
+    k, v = cache.gather(slots)
+    q = (30 * torch.randn(1, 4, 128, device="cuda")).to(dt)
+    table = torch.arange(7, device="cuda", dtype=torch.int32)[None].contiguous()
+    out = cache.attend(q, SM, table, torch.tensor([200], device="cuda", dtype=torch.int32))
+    torch.cuda.synchronize()
+    ref, _ = prompt_attention(_f64(q), _f64(k), _f64(v), SM)
+    size, _ = prompt_attention(_f64(q), _f64(k), np.abs(_f64(v)), SM)
+    # logits of magnitude up to 30 60 4 sqrt(128) sm ~ 1e4 have float32 errors of 1e4 2^-24 8: 5e-3 of a weight.  Where every value with
+    # a weight is 0 (4 bits), what is left is absolute: half a step of fp16's smallest numbers, 2^-25, above all that 200 weights
+    # below float32's smallest, 2^-126, add up to with values below 2^16 (2^-102).
+    assert (np.abs(_f64(out) - ref) <= 2.0 ** -11 * np.abs(ref) + (1.1 * 2.0 ** -11 + 1e-2) * size + 2.0 ** -25).all()
+
+
+@BOTH
+def test_nan_in_a_seen_token_reaches_its_own_heads_only(bits):
+    page = 16
+    pages, table, rows = _filled([50, 60], 2, page, bits, torch.float16, seed=12)
+    cache = tkv.PagedCache(n_q_heads=4, n_kv_heads=2, page_size=page, bits=bits, k_pages=pages[0], v_pages=pages[1])
+    q = torch.randn(2, 4, 128, device="cuda").half()
+    lens = torch.tensor([50, 60], device="cuda", dtype=torch.int32)
+    want = cache.attend(q, SM, table, lens)
+    bad = torch.full((1, 2, 128), 1.0, device="cuda").half()
+    bad[0, 1, 5] = float("nan")
+    slot = torch.from_numpy(paged.sequence_slots(table[1].cpu().numpy(), 60, page)[33:34].astype(np.int32)).cuda()
+    cache.append(None, bad, torch.ones_like(bad), slot)
+    out = cache.attend(q, SM, table, lens)
+    torch.cuda.synchronize()
+    assert torch.equal(out[0], want[0]) and out[1, 2:].isnan().all() and not out[1, :2].isnan().any()
+
+
+@BOTH
+def test_streams_threads_and_a_graph_over_a_growing_cache(bits):
+    """A captured decode step (append, attend) replays while lengths, slots and positions move on; eager calls of the same object on
+    another stream run beside it."""
+    from test_gpu_rope import _freq
+    page, hq, hkv, n_pages, b = 16, 8, 2, 12, 3
+    cache = tkv.PagedCache(n_q_heads=hq, n_kv_heads=hkv, page_size=page, bits=bits, n_pages=n_pages)
+    twin = tkv.PagedCache(n_q_heads=hq, n_kv_heads=hkv, page_size=page, bits=bits, n_pages=n_pages)
+    table = torch.randperm(n_pages, generator=torch.Generator().manual_seed(0)).to(torch.int32).view(b, 4).cuda()
+    f = _freq(128)
+    rows = torch.randn(b, hq + 2 * hkv, 128, device="cuda").half()
+    lens = torch.tensor([0, 20, 13], device="cuda", dtype=torch.int32)
+    for c in (cache, twin):
+        for i in range(b):
+            n = int(lens[i])
+            s = torch.from_numpy(paged.sequence_slots(table[i].cpu().numpy(), n, page).astype(np.int32)).cuda()
+            g = torch.Generator(device="cuda").manual_seed(i)
+            c.append(None, *(torch.randn(n, hkv, 128, generator=g, device="cuda").half() for _ in range(2)), s)
+
+    def step(c):
+        at = lens // page
+        slots = (table.gather(1, at[:, None].long())[:, 0] * page + lens % page).to(torch.int32)
+        q = c.append(rows[:, :hq], rows[:, hq:hq + hkv], rows[:, hq + hkv:], slots, lens, f)
+        return c.attend(q, SM, table, lens + 1, lse=True)
+
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        caught = step(cache)
+    side = torch.cuda.Stream()
+    for i in range(6):
+        graph.replay()
+        side.wait_stream(torch.cuda.current_stream())
+        with torch.cuda.stream(side):
+            want = step(twin)
+            beside = cache.attend(rows[:, :hq].contiguous(), SM, table, lens)
+        torch.cuda.synchronize()
+        assert torch.equal(caught[0], want[0]) and torch.equal(caught[1], want[1]), i
+        assert torch.equal(beside, cache.attend(rows[:, :hq].contiguous(), SM, table, lens))
+        lens += torch.tensor([1, 3, 2], device="cuda", dtype=torch.int32)    # (some slots are skipped: zeros there)
+        rows.mul_(0.9)
+
+
+def test_prompt_then_chunk_then_decode():
+    """As they are used: a prompt's rows normed, turned and put into 4-bit and 16-bit pages, a second chunk whose attention runs over the
+    gathered prefix, decode steps over the pages; the pages' attention agrees with the prompt attention over the gathered rows."""
+    from test_gpu_rope import _freq, _inputs
+    hq, hkv, page, n1, n2 = 8, 2, 32, 150, 61
+    f = _freq(128)
+    q, k, v, qw, kw = _inputs(n1 + n2 + 4, hq, hkv, torch.bfloat16, seed=1)
+    pos = torch.arange(n1 + n2 + 4, device="cuda", dtype=torch.int32)
+    a = dict(norm=True, q_weight=qw, k_weight=kw)
+    plan = tkv.PromptAttention(n_q_heads=hq, n_kv_heads=hkv)
+    for bits in (16, 4):
+        cache = tkv.PagedCache(n_q_heads=hq, n_kv_heads=hkv, page_size=page, bits=bits, n_pages=9)
+        table = torch.tensor([[7, 0, 3, 8, 1, 5, 2]], device="cuda", dtype=torch.int32)
+        slots = torch.from_numpy(paged.sequence_slots(table[0].cpu().numpy(), 224, page).astype(np.int32)).cuda()
+
+        def put(i, j):
+            return cache.append(q[i:j], k[i:j], v[i:j], slots[i:j], pos[i:j], f, **a)
+
+        def from_rows(x, n):
+            kk, vv = cache.gather(slots[:n])
+            return plan.attend(x, kk, vv, SM, [len(x)], [n], lse=True)
+
+        for i, j in ((0, n1), (n1, n1 + n2), *((n1 + n2 + s, n1 + n2 + s + 1) for s in range(4))):
+            x = put(i, j)
+            out, lse = cache.attend(x, SM, table, torch.tensor([j], device="cuda", dtype=torch.int32),
+                                    q_starts=torch.tensor([0, j - i], device="cuda", dtype=torch.int32), max_q_len=j - i, lse=True)
+            want, want_lse = from_rows(x, j)
+            torch.cuda.synchronize()
+            kk, vv = cache.gather(slots[:j])
+            _compare(out, lse, _f64(x), _f64(kk), _f64(vv), torch.float16)
+            assert (lse - want_lse).abs().max() <= 2e-5
