@@ -600,7 +600,9 @@ int32_t tkv_paged_append(const tkv_paged_desc* desc, const tkv_rope_desc* rope, 
 int32_t tkv_paged_gather(const tkv_paged_desc* desc, const void* k_pages, const void* v_pages, int32_t n_tokens, const int32_t* slots,
                          void* k_out, void* v_out, void* stream);
 
-/* Workspace bytes of tkv_paged_attn, whatever the call's sequences (any contents before a call). */
+/* Workspace bytes of tkv_paged_attn, whatever the call's sequences: partial results, and TKV_PAGED_COUNTERS bytes of counters at the
+ * end, which are ZERO-FILLED before its first use and left so by every call. */
+#define TKV_PAGED_COUNTERS 12288
 int32_t tkv_paged_attn_sizes(const tkv_paged_desc* desc, size_t* workspace_bytes);
 
 /*
@@ -610,7 +612,8 @@ int32_t tkv_paged_attn_sizes(const tkv_paged_desc* desc, size_t* workspace_bytes
  * [batch + 1], ascending; NULL: row b alone, n_tokens = batch).  Token i of n queries sees keys j <= i + k_lens[b] - n.
  * out = softmax(sm_scale q.k) v; a token that sees no key yields zeros, and -inf in lse.
  * q, out [n_tokens][Hq][128] contiguous; lse float32 [n_tokens][Hq] (natural logarithm of the sum of exponentials) or NULL.  Rows of out and
- * lse that belong to no sequence are left as they were.  max_q_len: the most queries that a sequence has, as the host knows it.
+ * lse that belong to no sequence (in front of the first, behind the last) are left as they were, or with clear_rest = 1 get zeros and
+ * -inf.  max_q_len: the most queries that a sequence has, as the host knows it.
  * Keys behind a sequence's last are never used, whatever their slots hold.  A page number outside the cache stands for rows of zeros; k_lens
  * beyond pages_each * page_size, or below 0, count as that, or as 0.
  * Products in desc->dtype with float32 sums (4 bits: of what the codes stand for, exactly); softmax statistics in float32.
@@ -620,8 +623,8 @@ int32_t tkv_paged_attn_sizes(const tkv_paged_desc* desc, size_t* workspace_bytes
  */
 int32_t tkv_paged_attn(const tkv_paged_desc* desc, const void* k_pages, const void* v_pages, int32_t batch, int32_t n_tokens,
                        int32_t max_q_len, const void* q, void* out, float* lse, const int32_t* page_table, int32_t pages_each,
-                       const int32_t* k_lens, const int32_t* q_starts, float sm_scale, void* workspace, size_t workspace_bytes,
-                       void* stream);
+                       const int32_t* k_lens, const int32_t* q_starts, int32_t clear_rest, float sm_scale, void* workspace,
+                       size_t workspace_bytes, void* stream);
 
 /* ---------------------------------------------------------------------------------
  * Offline identification (Sec. 4.1): which layers are quantization-friendly

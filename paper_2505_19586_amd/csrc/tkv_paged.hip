@@ -1,5 +1,6 @@
 // Paged caches: rows read back from their pages (tkv_paged_gather) and attention over them (tkv_paged_attn).
 #include <algorithm>
+#include <type_traits>
 
 #include "tkv_paged.h"
 
@@ -13,7 +14,6 @@ typedef short shortx4 __attribute__((ext_vector_type(4)));
 typedef _Float16 half8 __attribute__((ext_vector_type(8)));
 typedef __bf16 bhalf8 __attribute__((ext_vector_type(8)));
 typedef __attribute__((address_space(3))) char lds_char;
-
 
 struct GatherParams {
   tkv::Pages pages;
@@ -69,12 +69,14 @@ __global__ __launch_bounds__(256) void paged_gather_kernel(GatherParams p) {
   }
 }
 
-constexpr int kWaves = 4;        // of a workgroup
+constexpr int kWaves = 4;              // of a workgroup
 constexpr int kRowFloats = TKV_D + 4;  // of a row of partial sums in LDS (the four keep the banks apart)
 // Weights are 2^(logit - reference + kShift), and the reference follows a row's maximum only when that is 8 above it: at most 2^15, inside
 // fp16's range.
 constexpr float kShift = 7.f;
 constexpr float kNone = -3.402823466e38f;  // reference of a row without a key so far (finite: kNone - kNone is 0)
+constexpr int kMaxUnits = 256;             // compute units that the workspace has room for
+constexpr int kMostParts = 64;             // of an item (in workgroups), so that joining them stays short
 
 struct PagedParams {
   tkv::Pages pages;
@@ -84,85 +86,164 @@ struct PagedParams {
   const int32_t* table;
   const int32_t* k_lens;
   const int32_t* q_starts;  // NULL: a token of each sequence
-  float* parts;             // [2 per workgroup][rows of a tile][128] weighted sums
-  float* ml;                // [2 per workgroup][rows of a tile][2] (reference, sum)
+  float* parts;             // [2 per wave][rows of a tile][128] weighted sums
+  float* ml;                // [2 per wave][rows of a tile][2] (reference, sum)
+  uint32_t* arrivals;       // [wave] parts, of the item whose first cut lies behind its range, that have come in
   int32_t n_tokens, batch, hq, group, pages_each;
   int32_t workgroups;
-  float scale2;  // sm_scale * log2(e)
+  int32_t clear_rest;  // rows of no sequence get zeros
+  float scale2;        // sm_scale * log2(e)
 };
 
+// The kernel's arguments, read where they are used: kept in registers from the start on, they and the loop over the tiles have more than
+// there are.
+typedef const __attribute__((address_space(4))) PagedParams* Args;
+__device__ inline Args arguments() {
+  Args a = (Args)__builtin_amdgcn_kernarg_segment_ptr();
+  asm volatile("" : "+s"(a));
+  return a;
+}
+
 // How the work is shared out.  Every (sequence, KV head, tile of rows) is an item, its keys so many tiles of TK; all items' tiles in
-// a row are cut into as many equal ranges as there are workgroups.  Lengths lie on the device, so every workgroup works that out for
+// a row are cut into as many equal ranges as there are waves.  Lengths lie on the device, so every wave works that out for
 // itself: 64 sequences at a time, one a lane.
 struct Sequence {
   int32_t index, k_len, q_start, q_len, key_tiles, row_tiles;
   uint32_t first;  // of its tiles, among all
 };
 
+// One of an item's tiles, and the item.
+struct Place {
+  Sequence sq;
+  uint32_t start;     // of the item's tiles, among all
+  int32_t h, tile, t; // KV head, tile of rows, tile of keys
+};
+
 template <int TK, int ROWS>
 struct Walk {
-  const PagedParams& p;
-  int32_t chunk;       // first sequence of those at hand
+  int32_t group, batch;
+  int32_t chunk;                  // first sequence of those at hand
   int32_t k_len, q_start, q_len;  // per lane
   uint32_t first, count;          // per lane: tiles before its sequence, and of it
   uint32_t all;                   // tiles up to the chunk's end
+  int32_t longest;                // tiles of keys of the longest sequence so far
 
-  __device__ explicit Walk(const PagedParams& params) : p(params), chunk(0) { load(0, 0); }
+  __device__ Walk() : group(arguments()->group), batch(arguments()->batch), longest(1) { load(0, 0); }
 
   __device__ int32_t key_tiles(int32_t n) const { return max(1, (n + TK - 1) / TK); }
-  __device__ int32_t row_tiles(int32_t n) const { return (n * p.group + ROWS - 1) / ROWS; }
+  __device__ int32_t row_tiles(int32_t n) const { return (n * group + ROWS - 1) / ROWS; }
 
   __device__ void load(int32_t at, uint32_t before) {
-    const int lane = threadIdx.x % 64, b = min(at + lane, p.batch - 1);
+    const Args p = arguments();
+    const int lane = threadIdx.x % 64, b = at + lane;
     chunk = at;
-    k_len = (int32_t)max((int64_t)0, min((int64_t)p.k_lens[b], (int64_t)p.pages_each << p.pages.shift));
-    q_start = b;
-    q_len = 1;
-    if (p.q_starts) {
-      q_start = min(max(p.q_starts[b], 0), p.n_tokens);
-      q_len = max(0, min(p.q_starts[b + 1], p.n_tokens) - q_start);
+    k_len = q_start = q_len = 0;
+    if (b < batch) {
+      const int32_t* const starts = p->q_starts;
+      k_len = (int32_t)max((int64_t)0, min((int64_t)p->k_lens[b], (int64_t)p->pages_each << p->pages.shift));
+      q_start = b;
+      q_len = 1;
+      if (starts) {
+        q_start = min(max(starts[b], 0), p->n_tokens);
+        q_len = max(0, min(starts[b + 1], p->n_tokens) - q_start);
+      }
     }
-    count = at + lane < p.batch ? (uint32_t)(key_tiles(k_len) * row_tiles(q_len)) * (uint32_t)p.pages.hkv : 0u;
+    count = (uint32_t)(key_tiles(k_len) * row_tiles(q_len)) * (uint32_t)p->pages.hkv;  // (no rows: 0)
     uint32_t sum = count;
+    int32_t most = count ? key_tiles(k_len) : 1;
 #pragma unroll
     for (int d = 1; d < 64; d *= 2) {
       const uint32_t x = __shfl_up(sum, d, 64);
       if (lane >= d) sum += x;
+      most = max(most, __shfl_xor(most, d, 64));
     }
     first = before + sum - count;
     all = before + (uint32_t)__builtin_amdgcn_readlane((int)sum, 63);
+    longest = max(longest, __builtin_amdgcn_readfirstlane(most));
   }
   __device__ uint32_t total() {
-    while (chunk + 64 < p.batch) load(chunk + 64, all);
+    while (chunk + 64 < batch) load(chunk + 64, all);
     const uint32_t t = all;
     if (chunk != 0) load(0, 0);
     return t;
   }
-  // The sequence of tile number `at` (below total(), not before the chunk at hand); index -1 where there is none.
-  __device__ Sequence find(uint32_t at) {
-    while (at >= all && chunk + 64 < p.batch) load(chunk + 64, all);
-    // the last of those that begin at or before it (one without tiles shares its successor's beginning)
-    const int lane = threadIdx.x % 64;
-    const uint64_t before = __builtin_amdgcn_ballot_w64(count != 0u && first <= at && at < first + count);
-    Sequence s;
-    s.index = -1;
-    if (before == 0) return s;
-    const int l = 63 - __builtin_clzll(before);
-    (void)lane;
-    s.index = chunk + l;
-    s.k_len = __builtin_amdgcn_readlane(k_len, l);
-    s.q_start = __builtin_amdgcn_readlane(q_start, l);
-    s.q_len = __builtin_amdgcn_readlane(q_len, l);
-    s.first = (uint32_t)__builtin_amdgcn_readlane((int)first, l);
-    s.key_tiles = key_tiles(s.k_len);
-    s.row_tiles = row_tiles(s.q_len);
-    return s;
+  // The place of tile number `at` (not before the chunk at hand); sq.index -1 where there is none.
+  __device__ Place find(uint32_t at) {
+    while (at >= all && chunk + 64 < batch) load(chunk + 64, all);
+    const uint64_t here = __builtin_amdgcn_ballot_w64(first <= at && at < first + count);
+    Place x;
+    x.sq.index = -1;
+    if (here == 0) return x;
+    const int l = __builtin_ctzll(here);
+    x.sq.index = chunk + l;
+    x.sq.k_len = __builtin_amdgcn_readlane(k_len, l);
+    x.sq.q_start = __builtin_amdgcn_readlane(q_start, l);
+    x.sq.q_len = __builtin_amdgcn_readlane(q_len, l);
+    x.sq.first = (uint32_t)__builtin_amdgcn_readlane((int)first, l);
+    x.sq.key_tiles = key_tiles(x.sq.k_len);
+    x.sq.row_tiles = row_tiles(x.sq.q_len);
+    const uint32_t in = at - x.sq.first, item = in / (uint32_t)x.sq.key_tiles;
+    x.start = x.sq.first + item * (uint32_t)x.sq.key_tiles;
+    x.t = (int32_t)(at - x.start);
+    x.h = (int32_t)(item / (uint32_t)x.sq.row_tiles);
+    x.tile = (int32_t)(item - (uint32_t)x.h * (uint32_t)x.sq.row_tiles);
+    return x;
   }
 };
 
-// Tiles of a workgroup's range: as even as can be, and one for each wave at least.
-__device__ inline uint32_t range_of(uint32_t total, int workgroups) {
-  return max((uint32_t)kWaves, (total + (uint32_t)workgroups - 1) / (uint32_t)workgroups);
+// Tiles of a wave's range: as even as can be, but an item goes to about kMostParts workgroups at most.  (64 parts of one row join in about
+// 4 us; one sequence and one KV head would have 256.)
+__device__ inline uint32_t range_of(uint32_t total, int32_t longest, int workgroups) {
+  const uint32_t waves = (uint32_t)(kWaves * workgroups);
+  return max((total + waves - 1) / waves, (uint32_t)(longest + kWaves * kMostParts - 1) / (uint32_t)(kWaves * kMostParts));
+}
+
+// Where a wave's next sixteens of keys lie, one a lane: those of tiles begin, begin + (1 << log_step), ..., PER a tile, whatever items they are of.
+template <int PER>
+struct Plan {
+  uint32_t begin, stop;  // of the tiles at hand
+  int32_t log_step;      // the next tile is 1 << log_step on
+  // per lane
+  int64_t k_at, v_at;    // bytes from the pages' beginning: of the first row (16 bits; in 4 bits of the page's and head's block, v_at is k_at)
+  uint32_t place, rows;  // first place in the page, rows that are there
+
+  template <typename W>
+  __device__ void make(W& walk, uint32_t from, uint32_t end) {
+    const Args p = arguments();
+    while (from >= walk.all && walk.chunk + 64 < walk.batch) walk.load(walk.chunk + 64, walk.all);
+    begin = from;
+    stop = min(min(from + ((uint32_t)(64 / PER) << log_step), end), walk.all);
+    const int lane = threadIdx.x % 64;
+    const uint32_t g = min(from + ((uint32_t)(lane / PER) << log_step), stop - 1u);
+    int l = 0;  // the last sequence that begins at or before it (one without tiles shares its successor's beginning)
+#pragma unroll
+    for (int d = 32; d > 0; d /= 2) {
+      const uint32_t f = (uint32_t)__shfl((int)walk.first, l + d, 64);
+      if (f <= g) l += d;
+    }
+    const int32_t k_len = __shfl(walk.k_len, l, 64), q_len = __shfl(walk.q_len, l, 64);
+    const uint32_t first = (uint32_t)__shfl((int)walk.first, l, 64);
+    const uint32_t key_tiles = (uint32_t)walk.key_tiles(k_len), row_tiles = (uint32_t)max(1, walk.row_tiles(q_len));
+    const uint32_t in = g - first, item = in / key_tiles, h = min(item / row_tiles, (uint32_t)p->pages.hkv - 1u);
+    const int32_t key = 16 * ((int32_t)(in - item * key_tiles) * PER + lane % PER);
+    const int32_t there = max(0, min(16, k_len - key));
+    int32_t page = -1;
+    if (there > 0 && walk.chunk + l < walk.batch) page = p->table[(int64_t)(walk.chunk + l) * p->pages_each + (key >> p->pages.shift)];
+    const bool none = page < 0 || page >= p->pages.n_pages;
+    rows = none ? 0u : (uint32_t)there;
+    place = (uint32_t)(key & ((1 << p->pages.shift) - 1));
+    const int64_t id = none ? 0 : page, by = PER == 2 ? 2 : 1, first_row = PER == 2 ? place : 0;
+    k_at = (id * p->pages.k_sp + (int64_t)h * p->pages.k_sh + first_row * p->pages.k_st) * by;
+    if (PER == 2) v_at = (id * p->pages.v_sp + (int64_t)h * p->pages.v_sh + first_row * p->pages.v_st) * by;
+  }
+  __device__ bool has(uint32_t tile) const { return tile < stop; }
+  __device__ int lane_of(uint32_t tile) const { return (int)((tile - begin) >> log_step) * PER; }
+};
+
+// A lane's 64 bits, for all.
+__device__ inline int64_t of_lane(int64_t x, int l) {
+  const uint32_t lo = (uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)x, l), hi = (uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)((uint64_t)x >> 32), l);
+  return (int64_t)((uint64_t)hi << 32 | lo);
 }
 
 template <typename T>
@@ -193,7 +274,14 @@ __device__ inline void to_lds(__amdgpu_buffer_rsrc_t from, uint32_t to, uint32_t
   asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(to), "v"(lane_offset), "s"(from) : "memory");
 }
 
-// What a wave carries over a segment (some of an item's tiles): weighted sums, transposed (lane: row lane % 16 of each sixteen, channels
+// A descriptor of `bytes` bytes from an address that is the same for all lanes, as the assembly above wants it: in scalar registers.
+__device__ inline __amdgpu_buffer_rsrc_t uniform_array(const char* at, int32_t bytes) {
+  const uint64_t a = (uint64_t)at;
+  const uint64_t lo = (uint32_t)__builtin_amdgcn_readfirstlane((int)(uint32_t)a), hi = (uint32_t)__builtin_amdgcn_readfirstlane((int)(uint32_t)(a >> 32));
+  return __builtin_amdgcn_make_buffer_rsrc((void*)(hi << 32 | lo), 0, __builtin_amdgcn_readfirstlane(bytes), 0x00020000);
+}
+
+// What a wave carries over an item's tiles: weighted sums, transposed (lane: row lane % 16 of each sixteen, channels
 // 16 ct + 4 (lane / 16) + i), reference and its share of the sum of weights.
 template <int NT>
 struct Rows {
@@ -201,16 +289,19 @@ struct Rows {
   float ref[NT], sum[NT];
   int32_t limit[NT];  // last key that the lane's row sees
   int32_t limit_low;  // ... and the item's first row
+  float scale2;
 };
 
 // Weights of 16 Y keys from key0 on, from their logits s (lane: row, keys key0 + 16 y + 4 (lane / 16) + i) for the next product:
 // element 4 (y % 2) + i of operand y / 2.
 template <typename T, int NT, int Y>
-__device__ inline void weigh(Rows<NT>& r, floatx4 (&s)[NT][Y], uintx4 (&w)[NT][Y / 2], int key0, float scale2, int quarter) {
+__device__ inline void weigh(Rows<NT>& r, floatx4 (&s)[NT][Y], uintx4 (&w)[NT][Y / 2], int key0) {
+  const float scale2 = r.scale2;
   const bool mask = key0 + 16 * Y - 1 > r.limit_low;
+  const int quarter = threadIdx.x % 64 / 16;
 #pragma unroll
   for (int n = 0; n < NT; ++n) {
-    if (mask) {
+    if (__builtin_expect(mask, 0)) {
 #pragma unroll
       for (int y = 0; y < Y; ++y)
 #pragma unroll
@@ -222,7 +313,7 @@ __device__ inline void weigh(Rows<NT>& r, floatx4 (&s)[NT][Y], uintx4 (&w)[NT][Y
 #pragma unroll
       for (int i = 0; i < 4; ++i) top = fmaxf(top, s[n][y][i]);
     top *= scale2;
-    if (__builtin_amdgcn_ballot_w64(top > r.ref[n] + 8.f) != 0) {
+    if (__builtin_expect(__builtin_amdgcn_ballot_w64(top > r.ref[n] + 8.f) != 0, 0)) {
       top = tkv::over_rows(top, [](float a, float b) { return fmaxf(a, b); });
       const float next = fmaxf(r.ref[n], top), shrink = __builtin_amdgcn_exp2f(r.ref[n] - next);
       r.ref[n] = next;
@@ -243,84 +334,81 @@ __device__ inline void weigh(Rows<NT>& r, floatx4 (&s)[NT][Y], uintx4 (&w)[NT][Y
   }
 }
 
-// The pages of a wave's next 64 sixteens of keys, one a lane: those of its tiles t0, t0 + kWaves, ... of PER sixteens each.
-template <int PER>
-__device__ inline int32_t some_pages(const PagedParams& p, const Sequence& sq, int t0) {
-  const int lane = threadIdx.x % 64;
-  const int64_t key = 16 * ((int64_t)(t0 + kWaves * (lane / PER)) * PER + lane % PER);
-  const int64_t at = key >> p.pages.shift;
-  const int32_t id = key < sq.k_len ? p.table[(int64_t)sq.index * p.pages_each + at] : -1;
-  return id < p.pages.n_pages ? id : -1;
-}
-
 // A place of 16 bytes in a row of LDS: rows of 256 bytes keep their sixteen places in an order that depends on the row, so that the reads
 // (a column of keys; a 4 x 16 block of values) and writes meet all banks.
 __device__ inline int k_place(int row, int place) { return place ^ (row & 15); }
 __device__ inline int v_place(int row, int place) { return place ^ (((row & 7) << 1) | ((row >> 3) & 1)); }
+// Where a lane's transposing read of the first sixteen channels of sixteen values begins (channels 16 ct on: 32 ct in its bits 5 to 7, exclusive or).
+__device__ inline int v_read_at() {
+  const int lane = threadIdx.x % 64, col = lane % 16, row = 4 * (lane / 16) + col / 4;
+  return row * 256 + 16 * v_place(row, (col % 4) / 2) + 8 * (col % 2);
+}
+// Worked out anew where it is used, by one operation, rather than held in a register for each place.
+__device__ inline int anew(int x) {
+  asm volatile("" : "+v"(x));
+  return x;
+}
 
 // 16 bits: the bytes bound this.  Every wave takes tiles of 32 keys of its own through a ring of two in LDS, filled by loads that
-// do not pass through registers; no barrier until the waves join.
+// do not pass through registers.
 template <typename T, int NT>
-__device__ inline void segment16(const PagedParams& p, const Sequence& sq, int h, int t0, int t1, const uintx4 (&qf)[NT][4], Rows<NT>& r,
-                                 lds_char* ring) {
-  constexpr int kTile = 32 * TKV_D * 2;
-  const int lane = threadIdx.x % 64, col = lane % 16, quarter = lane / 16;
-  if (t0 >= t1) return;
+struct Tiles16 {
+  static constexpr int kKeys = 32, kPer = 2, kTile = kKeys * TKV_D * 2, kBytes = 4 * kTile;
+  lds_char* ring;
+  const char *k, *v;
+  int32_t k_st, v_st;  // bytes
   uint32_t k_off[4], v_off[4];
+  int turn;  // the half of the ring that the tile at hand is in
+  int ka, va;  // (of kk = 0 and ct = 0; the others differ in some bits: + 64 kk, + 32 ct without a carry)
+
+  __device__ Tiles16(lds_char* lds) : ring(lds), turn(0) {
+    const Args p = arguments();
+    k = (const char*)p->pages.k;
+    v = (const char*)p->pages.v;
+    k_st = (int32_t)(2 * p->pages.k_st);
+    v_st = (int32_t)(2 * p->pages.v_st);
+    const int lane = threadIdx.x % 64, col = lane % 16, quarter = lane / 16;
 #pragma unroll
-  for (int j = 0; j < 4; ++j) {
-    const int row = 4 * j + quarter;
-    k_off[j] = (uint32_t)(row * p.pages.k_st * 2) + 16u * (uint32_t)k_place(row, col);
-    v_off[j] = (uint32_t)(row * p.pages.v_st * 2) + 16u * (uint32_t)v_place(row, col);
+    for (int j = 0; j < 4; ++j) {
+      const int row = 4 * j + quarter;
+      k_off[j] = (uint32_t)(row * k_st) + 16u * (uint32_t)k_place(row, col);
+      v_off[j] = (uint32_t)(row * v_st) + 16u * (uint32_t)v_place(row, col);
+    }
+    ka = col * 256 + 16 * k_place(col, quarter);
+    va = v_read_at();
   }
-  const char* const k_head = (const char*)p.pages.k + (int64_t)h * p.pages.k_sh * 2;
-  const char* const v_head = (const char*)p.pages.v + (int64_t)h * p.pages.v_sh * 2;
-  const uint32_t ring0 = (uint32_t)(uintptr_t)ring;
-  int32_t pages = some_pages<2>(p, sq, t0);
-  int last = 0;  // the tile that `pages` begins with, in the wave's own count
-  const int mine = (t1 - t0 + kWaves - 1) / kWaves;
-  auto stage = [&](int n) {
-    const int t = t0 + kWaves * n;
+  static __device__ int q_channel(int kk) { return 32 * kk + 8 * (int)(threadIdx.x % 64 / 16); }
+
+  __device__ void stage(const Plan<kPer>& plan, uint32_t tile, int half) {
+    const uint32_t to0 = (uint32_t)(uintptr_t)ring + (uint32_t)(half * 2 * kTile);
 #pragma unroll
     for (int y = 0; y < 2; ++y) {
-      const int key = 32 * t + 16 * y, at = key & ((1 << p.pages.shift) - 1);
-      const int32_t id = __builtin_amdgcn_readlane(pages, 2 * (n - last) + y);
-      const int valid = id < 0 ? 0 : min(16, sq.k_len - key);  // rows behind the sequence's last, and pages outside, read as zeros
-      const int64_t page = max(id, 0);
-      const char* const kb = k_head + (page * p.pages.k_sp + at * p.pages.k_st) * 2;
-      const char* const vb = v_head + (page * p.pages.v_sp + at * p.pages.v_st) * 2;
-      const auto kr = __builtin_amdgcn_make_buffer_rsrc((void*)kb, 0, valid <= 0 ? 0 : (int)((valid - 1) * p.pages.k_st * 2 + TKV_D * 2), 0x00020000);
-      const auto vr = __builtin_amdgcn_make_buffer_rsrc((void*)vb, 0, valid <= 0 ? 0 : (int)((valid - 1) * p.pages.v_st * 2 + TKV_D * 2), 0x00020000);
-      const uint32_t to = ring0 + (uint32_t)((n & 1) * 2 * kTile + 4096 * y);
+      const int l = plan.lane_of(tile) + y, rows = __builtin_amdgcn_readlane((int)plan.rows, l);
+      // rows behind the sequence's last, and pages outside, read as zeros
+      const auto kr = uniform_array(k + of_lane(plan.k_at, l), rows == 0 ? 0 : (rows - 1) * k_st + TKV_D * 2);
+      const auto vr = uniform_array(v + of_lane(plan.v_at, l), rows == 0 ? 0 : (rows - 1) * v_st + TKV_D * 2);
+      const uint32_t to = to0 + 4096u * (uint32_t)y;
 #pragma unroll
       for (int j = 0; j < 4; ++j) to_lds(kr, to + 1024 * j, k_off[j]);
 #pragma unroll
       for (int j = 0; j < 4; ++j) to_lds(vr, to + kTile + 1024 * j, v_off[j]);
     }
-  };
-  lds_char* ka[4];
-  lds_char* va[8];
-#pragma unroll
-  for (int kk = 0; kk < 4; ++kk) ka[kk] = ring + (col * 256 + 16 * k_place(col, 4 * kk + quarter));
-  {
-    const int row = 4 * quarter + col / 4;
-#pragma unroll
-    for (int ct = 0; ct < 8; ++ct) va[ct] = ring + (kTile + row * 256 + 16 * v_place(row, 2 * ct + (col % 4) / 2) + 8 * (col % 2));
   }
-  stage(0);
-  for (int n = 0; n < mine; ++n) {
-    const int at = (n & 1) * 2 * kTile, key0 = 32 * (t0 + kWaves * n);
-    if (n + 1 - last == 32) {
-      last = n + 1;
-      pages = some_pages<2>(p, sq, t0 + kWaves * last);
-    }
+  __device__ void begin(const Plan<kPer>& plan, uint32_t tile) { stage(plan, tile, 0); }
+  // The tile that was sent for last, keys from key0 on; number `tile`, if there are more, is sent for with the plan that next() makes sure of.
+  template <typename Next>
+  __device__ void work(Plan<kPer>& plan, uint32_t tile, bool more, Next next, int key0, const uintx4 (&qf)[NT][4], Rows<NT>& r) {
+    lds_char* const at = ring + turn * 2 * kTile;
+    if (more) next();
     asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // (the other buffer's reads are done)
-    if (n + 1 < mine) {
-      stage(n + 1);
+    if (more) {
+      stage(plan, tile, turn ^ 1);
       asm volatile("s_waitcnt vmcnt(16)" ::: "memory");
     } else {
       asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
     }
+    const int k0 = anew(ka), v0 = anew(va);
+    turn ^= 1;
     floatx4 s[NT][2];
 #pragma unroll
     for (int m = 0; m < NT; ++m)
@@ -330,290 +418,449 @@ __device__ inline void segment16(const PagedParams& p, const Sequence& sq, int h
     for (int kk = 0; kk < 4; ++kk)
 #pragma unroll
       for (int y = 0; y < 2; ++y) {
-        const uintx4 a = lds_read16(ka[kk] + at + 4096 * y);
+        const uintx4 a = lds_read16(at + (k0 ^ 64 * kk) + 4096 * y);
 #pragma unroll
         for (int m = 0; m < NT; ++m) s[m][y] = mfma16<T>(a, qf[m][kk], s[m][y]);
       }
     uintx4 w[NT][1];
-    weigh<T, NT, 2>(r, s, w, key0, p.scale2, quarter);
+    weigh<T, NT, 2>(r, s, w, key0);
 #pragma unroll
     for (int ct = 0; ct < 8; ++ct) {
-      const uintx2 lo = lds_read_tr(va[ct] + at), hi = lds_read_tr(va[ct] + at + 4096);
+      const uintx2 lo = lds_read_tr(at + (v0 ^ 32 * ct) + kTile), hi = lds_read_tr(at + (v0 ^ 32 * ct) + kTile + 4096);
       const uintx4 a = __builtin_shufflevector(lo, hi, 0, 1, 2, 3);
 #pragma unroll
       for (int m = 0; m < NT; ++m) r.o[m][ct] = mfma16<T>(a, w[m][0], r.o[m][ct]);
     }
   }
-}
+};
 
 // 4 bits: tiles of 64 keys; codes go to registers (a lane has 32 channels of a key: one block, and eight channels for each of four
-// products, which do not mind the order of the channels), keys from there to the matrix cores, values, as numbers of the type, through LDS,
-// whose reads transpose them.
+// products, which do not mind the order of the channels), keys from there to the matrix cores, values, as numbers of the type, 32 keys at a
+// time through LDS, whose reads transpose them.  The next tile's codes are sent for as soon as this one's have left their registers.
 template <typename T, int NT>
-__device__ inline void segment4(const PagedParams& p, const Sequence& sq, int h, int t0, int t1, const uintx4 (&qf)[NT][4], Rows<NT>& r,
-                                lds_char* area) {
-  const int lane = threadIdx.x % 64, col = lane % 16, quarter = lane / 16;
-  if (t0 >= t1) return;
-  const int64_t block = (int64_t)(tkv::kRow4 + tkv::kScales4) << p.pages.shift;
-  const int scales = tkv::kRow4 << p.pages.shift;
-  int32_t pages = some_pages<4>(p, sq, t0);
-  int last = 0;
-  const int mine = (t1 - t0 + kWaves - 1) / kWaves;
-  struct Tile {
-    uintx4 k[4], v[4];
-    uint32_t ks[4], vs[4];
-  };
-  auto fetch = [&](int n, Tile& x) {
-    const int t = t0 + kWaves * n;
-#pragma unroll
-    for (int y = 0; y < 4; ++y) {
-      const int key = 64 * t + 16 * y, at = key & ((1 << p.pages.shift) - 1);
-      const int32_t id = __builtin_amdgcn_readlane(pages, 4 * (n - last) + y);
-      const int valid = id < 0 ? 0 : max(0, min(16, sq.k_len - key));
-      const int64_t off = ((int64_t)max(id, 0) * p.pages.hkv + h) * block;
-      // (rows behind the sequence's last have scales of 0, whatever their codes)
-      auto codes = [&](const void* base) { return __builtin_amdgcn_make_buffer_rsrc((char*)base + off + at * tkv::kRow4, 0, valid * tkv::kRow4, 0x00020000); };
-      auto scale = [&](const void* base) { return __builtin_amdgcn_make_buffer_rsrc((char*)base + off + scales + at * tkv::kScales4, 0, valid * tkv::kScales4, 0x00020000); };
-      x.k[y] = __builtin_amdgcn_raw_buffer_load_b128(codes(p.pages.k), col * 64 + quarter * 16, 0, 0);
-      x.ks[y] = __builtin_amdgcn_raw_buffer_load_b8(scale(p.pages.k), col * 4 + quarter, 0, 0);
-      x.v[y] = __builtin_amdgcn_raw_buffer_load_b128(codes(p.pages.v), col * 64 + quarter * 16, 0, 0);
-      x.vs[y] = __builtin_amdgcn_raw_buffer_load_b8(scale(p.pages.v), col * 4 + quarter, 0, 0);
-    }
-  };
-  lds_char* const row_at = area + col * 256;
-  int to[4];
-#pragma unroll
-  for (int i = 0; i < 4; ++i) to[i] = 16 * v_place(col, 4 * quarter + i);
-  lds_char* va[8];
-  {
-    const int row = 4 * quarter + col / 4;
-#pragma unroll
-    for (int ct = 0; ct < 8; ++ct) va[ct] = area + (row * 256 + 16 * v_place(row, 2 * ct + (col % 4) / 2) + 8 * (col % 2));
+struct Tiles4 {
+  static constexpr int kKeys = 64, kPer = 4, kBytes = 32 * TKV_D * 2;
+  lds_char* area;
+  const char *k_pages, *v_pages;
+  int32_t scales_at, block;  // bytes: where a block's scales begin, all of it
+  int to, va;  // (of i = 0 and ct = 0)
+  uintx4 k[4], v[4];
+  uint32_t ks[4], vs[4];
+
+  __device__ Tiles4(lds_char* lds) : area(lds) {
+    const Args p = arguments();
+    k_pages = (const char*)p->pages.k;
+    v_pages = (const char*)p->pages.v;
+    scales_at = tkv::kRow4 << p->pages.shift;
+    block = (tkv::kRow4 + tkv::kScales4) << p->pages.shift;
+    const int lane = threadIdx.x % 64, col = lane % 16, quarter = lane / 16;
+    to = col * 256 + 16 * v_place(col, 4 * quarter);
+    va = v_read_at();
   }
-  Tile x;
-  fetch(0, x);
-  for (int n = 0; n < mine; ++n) {
-    const int key0 = 64 * (t0 + kWaves * n);
-    if (n + 1 - last == 16) {
-      last = n + 1;
-      pages = some_pages<4>(p, sq, t0 + kWaves * last);
-    }
-    Tile now = x;
-    if (n + 1 < mine) fetch(n + 1, x);
-    floatx4 s[NT][4];
+  static __device__ int q_channel(int kk) { return 32 * (int)(threadIdx.x % 64 / 16) + 8 * kk; }
+
+  __device__ void fetch(const char* pages, const Plan<kPer>& plan, uint32_t tile, uintx4 (&codes)[4], uint32_t (&scales)[4]) {
+    const int lane = threadIdx.x % 64, col = lane % 16, quarter = lane / 16;
 #pragma unroll
     for (int y = 0; y < 4; ++y) {
+      const int l = plan.lane_of(tile) + y, rows = __builtin_amdgcn_readlane((int)plan.rows, l), place = __builtin_amdgcn_readlane((int)plan.place, l);
+      const auto from = uniform_array(pages + of_lane(plan.k_at, l), rows == 0 ? 0 : block);  // pages outside read as zeros
+      codes[y] = __builtin_amdgcn_raw_buffer_load_b128(from, col * tkv::kRow4 + quarter * 16, place * tkv::kRow4, 0);
+      // rows behind the sequence's last have scales of 0, whatever their codes
+      const int at = col < rows ? col * tkv::kScales4 + quarter : block;
+      scales[y] = __builtin_amdgcn_raw_buffer_load_b8(from, at, scales_at + place * tkv::kScales4, 0);
+    }
+  }
+  __device__ void begin(const Plan<kPer>& plan, uint32_t tile) {
+    fetch(k_pages, plan, tile, k, ks);
+    fetch(v_pages, plan, tile, v, vs);
+  }
+  template <typename Next>
+  __device__ void work(Plan<kPer>& plan, uint32_t tile, bool more, Next next, int key0, const uintx4 (&qf)[NT][4], Rows<NT>& r) {
+    const int to0 = anew(to), v0 = anew(va);
 #pragma unroll
-      for (int m = 0; m < NT; ++m) s[m][y] = (floatx4){0.f, 0.f, 0.f, 0.f};
-      const float scale = tkv::scale_of(now.ks[y]);
+    for (int z = 0; z < 2; ++z) {
+      floatx4 s[NT][2];
 #pragma unroll
-      for (int kk = 0; kk < 4; ++kk) {
-        const uintx4 a = __builtin_bit_cast(uintx4, tkv::values_of<T>(now.k[y][kk], scale));
+      for (int y = 0; y < 2; ++y) {
 #pragma unroll
-        for (int m = 0; m < NT; ++m) s[m][y] = mfma16<T>(a, qf[m][kk], s[m][y]);
+        for (int m = 0; m < NT; ++m) s[m][y] = (floatx4){0.f, 0.f, 0.f, 0.f};
+        const float scale = tkv::scale_of(ks[2 * z + y]);
+#pragma unroll
+        for (int kk = 0; kk < 4; ++kk) {
+          const uintx4 a = __builtin_bit_cast(uintx4, tkv::values_of<T>(k[2 * z + y][kk], scale));
+#pragma unroll
+          for (int m = 0; m < NT; ++m) s[m][y] = mfma16<T>(a, qf[m][kk], s[m][y]);
+        }
       }
-    }
+      if (z == 1 && more) {
+        next();
+        fetch(k_pages, plan, tile, k, ks);
+      }
 #pragma unroll
-    for (int y = 0; y < 4; ++y) {
-      const float scale = tkv::scale_of(now.vs[y]);
+      for (int y = 0; y < 2; ++y) {
+        const float scale = tkv::scale_of(vs[2 * z + y]);
 #pragma unroll
-      for (int i = 0; i < 4; ++i) lds_write16(row_at + 4096 * y + to[i], __builtin_bit_cast(uintx4, tkv::values_of<T>(now.v[y][i], scale)));
-    }
-    uintx4 w[NT][2];
-    weigh<T, NT, 4>(r, s, w, key0, p.scale2, quarter);
-    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
-#pragma unroll
-    for (int z = 0; z < 2; ++z)
+        for (int i = 0; i < 4; ++i) lds_write16(area + (to0 ^ 16 * i) + 4096 * y, __builtin_bit_cast(uintx4, tkv::values_of<T>(v[2 * z + y][i], scale)));
+      }
+      uintx4 w[NT][1];
+      weigh<T, NT, 2>(r, s, w, key0 + 32 * z);
+      __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
 #pragma unroll
       for (int ct = 0; ct < 8; ++ct) {
-        const uintx2 lo = lds_read_tr(va[ct] + 8192 * z), hi = lds_read_tr(va[ct] + 8192 * z + 4096);
+        const uintx2 lo = lds_read_tr(area + (v0 ^ 32 * ct)), hi = lds_read_tr(area + (v0 ^ 32 * ct) + 4096);
         const uintx4 a = __builtin_shufflevector(lo, hi, 0, 1, 2, 3);
 #pragma unroll
-        for (int m = 0; m < NT; ++m) r.o[m][ct] = mfma16<T>(a, w[m][z], r.o[m][ct]);
+        for (int m = 0; m < NT; ++m) r.o[m][ct] = mfma16<T>(a, w[m][0], r.o[m][ct]);
       }
-    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+      __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+    }
+    if (more) fetch(v_pages, plan, tile, v, vs);
+  }
+};
+
+template <typename T, int BITS, int NT>
+using Tiles = std::conditional_t<BITS == 16, Tiles16<T, NT>, Tiles4<T, NT>>;
+
+// Workgroups of a compute unit: what registers and LDS have room for.  LDS: the waves' rings or areas, and the waves' results where they join.
+template <int BITS, int NT>
+constexpr int workgroups_each() { return BITS == 16 ? 1 : 2; }
+template <typename T, int BITS, int NT>
+constexpr int lds_bytes() {
+  return std::max(kWaves * Tiles<T, BITS, NT>::kBytes, kWaves * 16 * (kRowFloats + 2) * 4 + 16);
+}
+
+// Zeros, and -inf, for rows in front of the first sequence and behind the last.
+template <typename T>
+__device__ inline void clear_rows_of_no_sequence() {
+  const Args p = arguments();
+  const int front = min(max(p->q_starts[0], 0), p->n_tokens), back = min(max(p->q_starts[p->batch], front), p->n_tokens);
+  const int none = front + p->n_tokens - back, row_places = p->hq * TKV_D / 8;
+  for (int i = blockIdx.x; i < none; i += gridDim.x) {
+    const int64_t token = i < front ? i : back + (i - front);
+    for (int c = threadIdx.x; c < row_places; c += 64 * kWaves) ((uintx4*)p->out)[token * row_places + c] = (uintx4){0u, 0u, 0u, 0u};
+    for (int c = threadIdx.x; p->lse && c < p->hq; c += 64 * kWaves) p->lse[token * p->hq + c] = -INFINITY;
   }
 }
 
-template <typename T>
-__device__ inline void store8(T* to, floatx8 x) { *(uintx4*)to = pack8<T>(x); }
+// An item's parts.  A workgroup whose whole range lies in one item joins its waves' results itself and has one part (slot 8 g); elsewhere
+// every wave has its own: slot 2 w for one that begins with the wave's range, 2 w + 1 otherwise.
+struct Parts {
+  uint32_t start, pw;           // the item's first tile, tiles of a wave's range
+  int32_t w0, g0, g1;           // first wave, first and last workgroup
+  bool one0, one1;              // these have one part each
+  int32_t head, middle, count;  // parts of the first workgroup, of those between, all
 
-// Keys of a tile, and bytes of LDS: the waves' rings or areas, and the waves' results where they join.
-template <int BITS>
-constexpr int tile_keys() { return BITS == 16 ? 32 : 64; }
-template <int BITS, int NT>
-constexpr int lds_bytes() {
-  return std::max(kWaves * (BITS == 16 ? 4 * 32 * TKV_D * 2 : 64 * TKV_D * 2), kWaves * 16 * NT * (kRowFloats + 2) * 4);
+  __device__ Parts(const Place& x, uint32_t range, uint32_t total) : start(x.start), pw(range) {
+    const uint32_t end = x.start + (uint32_t)x.sq.key_tiles;
+    const int32_t w1 = (int32_t)((end - 1) / pw);
+    w0 = (int32_t)(start / pw);
+    g0 = w0 / kWaves;
+    g1 = w1 / kWaves;
+    one0 = within(g0, end, total);
+    one1 = within(g1, end, total);
+    head = one0 ? 1 : min(w1, kWaves * g0 + kWaves - 1) - w0 + 1;
+    middle = max(0, g1 - g0 - 1);
+    count = head + middle + (g1 == g0 ? 0 : one1 ? 1 : w1 - kWaves * g1 + 1);
+  }
+  __device__ bool within(int32_t g, uint32_t end, uint32_t total) const {  // the workgroup's range in the item
+    const uint64_t a = (uint64_t)g * kWaves * pw;
+    return start <= a && end >= min((uint64_t)total, a + (uint64_t)kWaves * pw);
+  }
+  __device__ int32_t slot(int32_t i) const {
+    if (i < head) {
+      const int32_t w = w0 + i;
+      return one0 ? 2 * kWaves * g0 : 2 * w + (i == 0 && start > (uint32_t)w * pw ? 1 : 0);
+    }
+    if (i < head + middle) return 2 * kWaves * (g0 + 1 + i - head);
+    return 2 * (kWaves * g1 + (one1 ? 0 : i - head - middle));
+  }
+};
+
+// Parts cross workgroups through stores and loads that pass by the caches that are not coherent between them ("sc1").
+template <int ROWS>
+struct PartStore {
+  __amdgpu_buffer_rsrc_t o, ml;
+  __device__ explicit PartStore(Args p)
+      : o(__builtin_amdgcn_make_buffer_rsrc(p->parts, 0, (int)((uint32_t)(2 * kWaves * p->workgroups) * (ROWS * TKV_D * 4u)), 0x00020000)),
+        ml(__builtin_amdgcn_make_buffer_rsrc(p->ml, 0, (int)((uint32_t)(2 * kWaves * p->workgroups) * (ROWS * 8u)), 0x00020000)) {}
+  __device__ void put(int slot, int row, int c, floatx4 x) const {
+    __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(uintx4, x), o, (uint32_t)((slot * ROWS + row) * TKV_D + c) * 4u, 0, 16);
+  }
+  __device__ void put(int slot, int row, float ref, float sum) const {
+    const float2 x = make_float2(ref, sum);
+    __builtin_amdgcn_raw_buffer_store_b64(__builtin_bit_cast(uintx2, x), ml, (uint32_t)(slot * ROWS + row) * 8u, 0, 16);
+  }
+};
+
+// Where a finished row of an item goes, and the logarithm of its sum.
+__device__ inline int64_t row_out(Args p, const Place& x, int row) {
+  const int group = p->group, token = row / group, head = row - token * group;
+  return (int64_t)(x.sq.q_start + token) * p->hq + x.h * group + head;
+}
+__device__ inline float log_sum(float ref, float sum) {
+  return sum == 0.f ? -INFINITY : (ref - kShift + __builtin_amdgcn_logf(sum)) * 0.69314718055994531f;
+}
+
+// A wave joins an item's parts for some of its rows: row0, row0 + step, ...  A row's parts are shared out over the wave's four sixteens of
+// lanes, a lane has eight channels.  Four loads are on their way at once, of four rows where there are no more than four parts.
+// What is added up in which order depends on the number of parts alone: the same bits, whoever comes last.
+template <typename T, int ROWS>
+__device__ inline void join_rows(Args p, const Place& x, const Parts& parts, int row0, int step) {
+  constexpr int kAtOnce = 4;
+  const int lane = threadIdx.x % 64, share = lane / 16, c = 8 * (lane % 16);
+  const int rows = min(ROWS, x.sq.q_len * p->group - ROWS * x.tile), rounds = (parts.count + 3) / 4;
+  const tkv::AgentBuf ob(p->parts, (uint32_t)(2 * kWaves * p->workgroups) * (ROWS * TKV_D * 4u));
+  const tkv::AgentBuf mb(p->ml, (uint32_t)(2 * kWaves * p->workgroups) * (ROWS * 8u));
+  float m = kNone, l = 0.f;
+  floatx8 acc = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+  int row = row0, round = 0;
+#pragma nounroll
+  while (row < rows) {
+    tkv::tkv_u32x2 st[kAtOnce];
+    tkv::tkv_u32x4 lo[kAtOnce], hi[kAtOnce];
+    int r = row, n = round;
+#pragma unroll
+    for (int y = 0; y < kAtOnce; ++y) {
+      const int i = 4 * n + share;
+      const uint32_t at = (uint32_t)(parts.slot(min(i, parts.count - 1)) * ROWS + r);
+      const bool there = i < parts.count && r < rows;  // (absent ones are zeros)
+      st[y] = mb.x2(there ? at * 8u : tkv::AgentBuf::kNone);
+      lo[y] = ob.x4(there ? (at * TKV_D + c) * 4u : tkv::AgentBuf::kNone);
+      hi[y] = ob.x4(there ? (at * TKV_D + c) * 4u + 16u : tkv::AgentBuf::kNone);
+      if (++n == rounds) n = 0, r += step;
+    }
+#pragma unroll
+    for (int y = 0; y < kAtOnce; ++y) {
+      if (row >= rows) break;
+      const uint32_t ref_bits = st[y].x, sum_bits = st[y].y;
+      const float ref = 4 * round + share < parts.count ? __builtin_bit_cast(float, ref_bits) : kNone;
+      const float top = fmaxf(m, ref), shrink = __builtin_amdgcn_exp2f(m - top), w = __builtin_amdgcn_exp2f(ref - top);
+      m = top;
+      l = __builtin_fmaf(__builtin_bit_cast(float, sum_bits), w, l * shrink);
+      const floatx4 a = __builtin_bit_cast(floatx4, lo[y]), b = __builtin_bit_cast(floatx4, hi[y]);
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        acc[k] = __builtin_fmaf(a[k], w, acc[k] * shrink);
+        acc[4 + k] = __builtin_fmaf(b[k], w, acc[4 + k] * shrink);
+      }
+      if (++round < rounds) continue;
+      // the row's last: the four sixteens together
+      auto max2 = [](float u, float v) { return fmaxf(u, v); };
+      auto add = [](float u, float v) { return u + v; };
+      const float all = tkv::over_rows(m, max2), mine = __builtin_amdgcn_exp2f(m - all), sum = tkv::over_rows(l * mine, add);
+      const float inv = sum == 0.f ? 0.f : 1.f / sum;  // (no key: zeros)
+#pragma unroll
+      for (int k = 0; k < 8; ++k) acc[k] = tkv::over_rows(acc[k] * mine, add) * inv;
+      const int64_t to = row_out(p, x, ROWS * x.tile + row);
+      if (share == 0) *(uintx4*)((T*)p->out + to * TKV_D + c) = pack8<T>(acc);
+      if (p->lse && lane == 0) p->lse[to] = log_sum(all, sum);
+      m = kNone;
+      l = 0.f;
+      acc = (floatx8){0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+      round = 0;
+      row += step;
+    }
+  }
 }
 
 template <typename T, int BITS, int NT>
-__global__ __launch_bounds__(64 * kWaves, BITS == 4 && NT < 4 ? 2 : 1) void paged_attn_kernel(PagedParams p) {
+__global__ __launch_bounds__(64 * kWaves, 2) void paged_attn_kernel(PagedParams) {
   extern __shared__ __attribute__((aligned(1024))) char lds[];
-  constexpr int kRows = 16 * NT, TK = tile_keys<BITS>();
+  typedef Tiles<T, BITS, NT> Tile;
+  constexpr int kRows = 16 * NT;
   const int lane = threadIdx.x % 64, col = lane % 16, quarter = lane / 16;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
-  Walk<TK, kRows> walk(p);
-  const uint32_t total = walk.total(), per = range_of(total, p.workgroups);
-  const uint64_t begin64 = (uint64_t)blockIdx.x * per;
-  if (begin64 >= total) return;
-  const uint32_t begin = (uint32_t)begin64, end = (uint32_t)min((uint64_t)total, begin64 + per);
-  for (uint32_t at = begin; at < end;) {
-    const Sequence sq = walk.find(at);
-    if (sq.index < 0) return;
-    const uint32_t in = at - sq.first, item = in / (uint32_t)sq.key_tiles;
-    const int a = (int)(in - item * (uint32_t)sq.key_tiles);
-    const int b = (int)min((uint32_t)sq.key_tiles, (uint32_t)a + (end - at));
-    const int h = (int)(item / (uint32_t)sq.row_tiles), tile = (int)(item - (uint32_t)h * (uint32_t)sq.row_tiles);
-    const int rows = sq.q_len * p.group, ahead = sq.k_len - sq.q_len;
+  tkv::fetch_arguments<sizeof(PagedParams)>();
+  Walk<Tile::kKeys, kRows> walk;
+  const uint32_t total = walk.total(), pw = range_of(total, walk.longest, arguments()->workgroups);
+  if (arguments()->clear_rest) clear_rows_of_no_sequence<T>();
+  const uint64_t group_begin = (uint64_t)blockIdx.x * kWaves * pw;
+  if (group_begin >= total) return;
+  const uint64_t begin64 = group_begin + (uint64_t)wave * pw;
+  uint32_t begin = (uint32_t)min((uint64_t)total, begin64), end = (uint32_t)min((uint64_t)total, begin64 + pw);
 
-    Rows<NT> r;
-    uintx4 qf[NT][4];
-    r.limit_low = tile * kRows / p.group + ahead;
+  Place x = walk.find(begin < end ? begin : (uint32_t)group_begin);
+  // Whether the workgroup's whole range lies in one item (all its waves find the same): then they take its tiles in turn, and join before
+  // they hand on.
+  const bool together = x.sq.index >= 0 && x.start <= (uint32_t)group_begin &&
+                        (uint64_t)x.start + (uint32_t)x.sq.key_tiles >= min((uint64_t)total, group_begin + (uint64_t)kWaves * pw);
+
+  Rows<NT> r;
+  uintx4 qf[NT][4];
+  auto open = [&](const Place& at) {  // an item's rows, and where their keys end
+    const Args p = arguments();
+    const int rows = at.sq.q_len * walk.group;
 #pragma unroll
     for (int m = 0; m < NT; ++m) {
-      const int row = min(tile * kRows + 16 * m + col, rows - 1), token = row / p.group, head = row - token * p.group;
-      r.limit[m] = token + ahead;
+      const T* const q = (const T*)p->q + row_out(p, at, min(at.tile * kRows + 16 * m + col, rows - 1)) * TKV_D;
+#pragma unroll
+      for (int kk = 0; kk < 4; ++kk) qf[m][kk] = *(const uintx4*)(q + Tile::q_channel(kk));
+    }
+  };
+  auto reset = [&](const Place& at) {
+    const int rows = at.sq.q_len * walk.group, ahead = at.sq.k_len - at.sq.q_len;
+    r.scale2 = arguments()->scale2;
+    r.limit_low = at.tile * kRows / walk.group + ahead;
+#pragma unroll
+    for (int m = 0; m < NT; ++m) {
+      const int row = min(at.tile * kRows + 16 * m + col, rows - 1);
+      r.limit[m] = row / walk.group + ahead;
       r.ref[m] = kNone;
       r.sum[m] = 0.f;
 #pragma unroll
       for (int ct = 0; ct < 8; ++ct) r.o[m][ct] = (floatx4){0.f, 0.f, 0.f, 0.f};
-      const T* const q = (const T*)p.q + ((int64_t)(sq.q_start + token) * p.hq + h * p.group + head) * TKV_D;
-#pragma unroll
-      for (int kk = 0; kk < 4; ++kk) qf[m][kk] = *(const uintx4*)(q + (BITS == 16 ? 32 * kk + 8 * quarter : 32 * quarter + 8 * kk));
-#pragma unroll
-      for (int kk = 0; kk < 4; ++kk) asm volatile("" : "+v"(qf[m][kk]));  // (waited for here, not in the loop)
     }
-    if constexpr (BITS == 16) segment16<T, NT>(p, sq, h, a + wave, b, qf, r, (lds_char*)lds + wave * (4 * 32 * TKV_D * 2));
-    else segment4<T, NT>(p, sq, h, a + wave, b, qf, r, (lds_char*)lds + wave * (64 * TKV_D * 2));
-
-    // the waves join: everyone's results into LDS, then sixteen threads a row
-    asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");  // no load may land after the ring is used otherwise
-    __syncthreads();
-    float* const o_s = (float*)lds;                              // [wave][row][kRowFloats]
-    float* const ml_s = o_s + kWaves * kRows * kRowFloats;       // [wave][row][2]
+    // (The rows are waited for here: the compiler, which does not know of the loads to LDS, would wait for them and those inside
+    // the loop.)
 #pragma unroll
-    for (int m = 0; m < NT; ++m) {
-      const float sum = tkv::over_rows(r.sum[m], [](float x, float y) { return x + y; });
-      const int at_row = wave * kRows + 16 * m + col;
+    for (int m = 0; m < NT; ++m)
 #pragma unroll
-      for (int ct = 0; ct < 8; ++ct) *(floatx4*)(o_s + at_row * kRowFloats + 16 * ct + 4 * quarter) = r.o[m][ct];
-      if (quarter == 0) *(float2*)(ml_s + 2 * at_row) = make_float2(r.ref[m], sum);
+      for (int kk = 0; kk < 4; ++kk) asm volatile("" : "+v"(qf[m][kk]));
+  };
+  if (together) {
+    begin = (uint32_t)min((uint64_t)total, group_begin + (uint64_t)wave);
+    end = (uint32_t)min((uint64_t)total, group_begin + (uint64_t)kWaves * pw);
+  }
+  if (x.sq.index < 0 || (!together && begin >= end)) return;  // (the first not with ascending q_starts)
+  Tile tiles((lds_char*)lds + wave * Tile::kBytes);
+  Plan<Tile::kPer> plan;
+  plan.log_step = together ? 2 : 0;
+  static_assert(kWaves == 4, "log_step");
+  const uint32_t step = 1u << plan.log_step;
+  open(x);
+  if (begin < end) {
+    plan.make(walk, begin, end);
+    tiles.begin(plan, begin);
+  }
+  reset(x);
+  for (uint32_t at = begin;;) {
+    const uint32_t stop = min(end, x.start + (uint32_t)x.sq.key_tiles);
+    const bool begins = at == begin;
+    for (; at < stop; at += step)
+      tiles.work(plan, at + step, at + step < end, [&] { if (__builtin_expect(!plan.has(at + step), 0)) plan.make(walk, at + step, end); },
+                 Tile::kKeys * (int)(at - x.start), qf, r);
+    const Place done = x;
+    bool last = together || at >= end;
+    if (!last) {  // the next item's rows are on their way while this one's results leave
+      x = walk.find(at);
+      last = x.sq.index < 0;
+      if (!last) open(x);
     }
-    __syncthreads();
-    const bool whole = a == 0 && b == sq.key_tiles;
-    const int slot = 2 * (int)blockIdx.x + (at == begin ? 0 : 1);
+    const Args p = arguments();
+    const Parts parts(done, pw, total);
+    const PartStore<kRows> store(p);
+    const int rows = done.sq.q_len * walk.group;
+    bool joins = false;
+    if (!together) {
+      const int slot = 2 * (kWaves * (int)blockIdx.x + wave) + (begins ? 0 : 1);
 #pragma unroll
-    for (int m = 0; m < NT; ++m) {
-      const int in_tile = 16 * m + threadIdx.x / 16, row = tile * kRows + in_tile, c = 8 * (threadIdx.x % 16);
-      if (row >= rows) continue;
-      float f[kWaves], top = kNone, sum = 0.f;
+      for (int m = 0; m < NT; ++m) {
+        const float sum = tkv::over_rows(r.sum[m], [](float a, float b) { return a + b; });
+        const int row = done.tile * kRows + 16 * m + col;
+        if (row >= rows) continue;
+        if (parts.count == 1) {
+          typedef T T4 __attribute__((ext_vector_type(4)));
+          const int64_t to = row_out(p, done, row);
+          const float inv = sum == 0.f ? 0.f : 1.f / sum;  // (no key: zeros)
 #pragma unroll
-      for (int w = 0; w < kWaves; ++w) top = fmaxf(top, f[w] = ml_s[2 * (w * kRows + in_tile)]);
-      floatx8 x = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+          for (int ct = 0; ct < 8; ++ct) *(T4*)((T*)p->out + to * TKV_D + 16 * ct + 4 * quarter) = __builtin_convertvector(r.o[m][ct] * inv, T4);
+          if (p->lse && quarter == 0) p->lse[to] = log_sum(r.ref[m], sum);
+        } else {
 #pragma unroll
-      for (int w = 0; w < kWaves; ++w) {
-        f[w] = __builtin_amdgcn_exp2f(f[w] - top);
-        sum = __builtin_fmaf(ml_s[2 * (w * kRows + in_tile) + 1], f[w], sum);
-        const float* const from = o_s + (w * kRows + in_tile) * kRowFloats + c;
-#pragma unroll
-        for (int i = 0; i < 8; ++i) x[i] = __builtin_fmaf(from[i], f[w], x[i]);
+          for (int ct = 0; ct < 8; ++ct) store.put(slot, 16 * m + col, 16 * ct + 4 * quarter, r.o[m][ct]);
+          if (quarter == 0) store.put(slot, 16 * m + col, r.ref[m], sum);
+        }
       }
-      if (!whole) {
-        float* const to = p.parts + ((size_t)slot * kRows + in_tile) * TKV_D + c;
-        *(floatx4*)to = __builtin_shufflevector(x, x, 0, 1, 2, 3);
-        *(floatx4*)(to + 4) = __builtin_shufflevector(x, x, 4, 5, 6, 7);
-        if (c == 0) *(float2*)(p.ml + ((size_t)slot * kRows + in_tile) * 2) = make_float2(top, sum);
-        continue;
+      if (parts.count > 1) {
+        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");  // the part is in memory before the count goes up
+        uint32_t before = 0;
+        if (lane == 0) before = atomicAdd(p->arrivals + parts.w0, 1u);
+        joins = (uint32_t)__builtin_amdgcn_readfirstlane((int)before) == (uint32_t)parts.count - 1u;
       }
-      const int token = row / p.group, head = row - token * p.group;
-      const int64_t to = (int64_t)(sq.q_start + token) * p.hq + h * p.group + head;
-      store8<T>((T*)p.out + to * TKV_D + c, x * (sum == 0.f ? 0.f : 1.f / sum));  // (no key: zeros)
-      if (p.lse && c == 0) p.lse[to] = sum == 0.f ? -INFINITY : (top - kShift + __builtin_amdgcn_logf(sum)) * 0.69314718055994531f;
+    } else {
+      // the waves join, sixteen rows at a time: everyone's results into LDS, then sixteen threads a row
+      asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");  // no load may land after the ring is used otherwise
+      float* const o_s = (float*)lds;                      // [wave][row][kRowFloats]
+      float* const ml_s = o_s + kWaves * 16 * kRowFloats;  // [wave][row][2]
+#pragma unroll
+      for (int m = 0; m < NT; ++m) {
+        const float part = tkv::over_rows(r.sum[m], [](float a, float b) { return a + b; });
+        __syncthreads();
+#pragma unroll
+        for (int ct = 0; ct < 8; ++ct) *(floatx4*)(o_s + (16 * wave + col) * kRowFloats + 16 * ct + 4 * quarter) = r.o[m][ct];
+        if (quarter == 0) *(float2*)(ml_s + 2 * (16 * wave + col)) = make_float2(r.ref[m], part);
+        __syncthreads();
+        const int at_row = threadIdx.x / 16, in_tile = 16 * m + at_row, row = done.tile * kRows + in_tile, c = 8 * (threadIdx.x % 16);
+        if (row >= rows) continue;
+        float f[kWaves], top = kNone, sum = 0.f;
+#pragma unroll
+        for (int w = 0; w < kWaves; ++w) top = fmaxf(top, f[w] = ml_s[2 * (16 * w + at_row)]);
+        floatx8 acc = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int w = 0; w < kWaves; ++w) {
+          f[w] = __builtin_amdgcn_exp2f(f[w] - top);
+          sum = __builtin_fmaf(ml_s[2 * (16 * w + at_row) + 1], f[w], sum);
+          const float* const from = o_s + (16 * w + at_row) * kRowFloats + c;
+#pragma unroll
+          for (int i = 0; i < 8; ++i) acc[i] = __builtin_fmaf(from[i], f[w], acc[i]);
+        }
+        if (parts.count > 1) {
+          const int slot = 2 * kWaves * (int)blockIdx.x;
+          store.put(slot, in_tile, c, __builtin_shufflevector(acc, acc, 0, 1, 2, 3));
+          store.put(slot, in_tile, c + 4, __builtin_shufflevector(acc, acc, 4, 5, 6, 7));
+          if (c == 0) store.put(slot, in_tile, top, sum);
+          continue;
+        }
+        const int64_t to = row_out(p, done, row);
+        *(uintx4*)((T*)p->out + to * TKV_D + c) = pack8<T>(acc * (sum == 0.f ? 0.f : 1.f / sum));  // (no key: zeros)
+        if (p->lse && c == 0) p->lse[to] = log_sum(top, sum);
+      }
+      if (parts.count > 1) {
+        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");  // the part is in memory before the count goes up
+        __syncthreads();
+        uint32_t* const flag = (uint32_t*)(ml_s + 2 * kWaves * 16);
+        if (threadIdx.x == 0) *flag = atomicAdd(p->arrivals + parts.w0, 1u);
+        __syncthreads();
+        joins = *flag == (uint32_t)parts.count - 1u;
+      }
     }
-    __syncthreads();
-    at += (uint32_t)(b - a);
+    if (joins) {
+      if (lane == 0) __hip_atomic_store(p->arrivals + parts.w0, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+      join_rows<T, kRows>(p, done, parts, together ? wave : 0, together ? kWaves : 1);
+    }
+    if (last) return;
+    reset(x);
   }
 }
 
-// Joins the parts of items that were cut: workgroup w looks after the item, if there is one, whose first cut lies behind range w, a wave a
-// row, a lane two channels.
-template <typename T, int BITS, int NT>
-__global__ __launch_bounds__(256) void paged_merge_kernel(PagedParams p) {
-  constexpr int kRows = 16 * NT;
-  const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
-  Walk<tile_keys<BITS>(), kRows> walk(p);
-  const uint32_t total = walk.total(), per = range_of(total, p.workgroups);
-  const uint64_t cut = (uint64_t)(blockIdx.x + 1) * per;
-  if (cut >= total) return;
-  const Sequence sq = walk.find((uint32_t)cut);
-  if (sq.index < 0) return;
-  const uint32_t in = (uint32_t)cut - sq.first, item = in / (uint32_t)sq.key_tiles;
-  const uint32_t start = sq.first + item * (uint32_t)sq.key_tiles;
-  if (start >= cut || start < cut - per) return;
-  const int h = (int)(item / (uint32_t)sq.row_tiles), tile = (int)(item - (uint32_t)h * (uint32_t)sq.row_tiles);
-  const int in_tile = 4 * blockIdx.y + wave, row = tile * kRows + in_tile;
-  if (row >= sq.q_len * p.group) return;
-  const int parts = (int)((start + (uint32_t)sq.key_tiles - 1) / per - blockIdx.x) + 1;
-  const int first_slot = 2 * (int)blockIdx.x + (start == cut - per ? 0 : 1);
-  float m = kNone, l = 0.f;
-  float2 acc = make_float2(0.f, 0.f);
-  // (requests of eight parts at a time, absent ones those of the first with a weight of zero)
-  for (int i0 = 0; i0 < parts; i0 += 8) {
-    float2 st[8], v[8];
-#pragma unroll
-    for (int y = 0; y < 8; ++y) {
-      const int i = i0 + y < parts ? i0 + y : 0;
-      const size_t at = (size_t)(i == 0 ? first_slot : 2 * ((int)blockIdx.x + i)) * kRows + in_tile;
-      st[y] = *(const float2*)(p.ml + at * 2);
-      v[y] = *(const float2*)(p.parts + at * TKV_D + 2 * lane);
-    }
-    float top = m;
-#pragma unroll
-    for (int y = 0; y < 8; ++y) top = fmaxf(top, st[y].x);
-    const float shrink = __builtin_amdgcn_exp2f(m - top);
-    m = top;
-    l *= shrink;
-    acc.x *= shrink;
-    acc.y *= shrink;
-#pragma unroll
-    for (int y = 0; y < 8; ++y) {
-      const float w = i0 + y < parts ? __builtin_amdgcn_exp2f(st[y].x - m) : 0.f;
-      l = __builtin_fmaf(st[y].y, w, l);
-      acc.x = __builtin_fmaf(v[y].x, w, acc.x);
-      acc.y = __builtin_fmaf(v[y].y, w, acc.y);
-    }
-  }
-  const int token = row / p.group, head = row - token * p.group;
-  const int64_t to = (int64_t)(sq.q_start + token) * p.hq + h * p.group + head;
-  typedef T T2 __attribute__((ext_vector_type(2)));
-  const float inv = l == 0.f ? 0.f : 1.f / l;
-  *(T2*)((T*)p.out + to * TKV_D + 2 * lane) = (T2){(T)(acc.x * inv), (T)(acc.y * inv)};
-  if (p.lse && lane == 0) p.lse[to] = l == 0.f ? -INFINITY : (m - kShift + __builtin_amdgcn_logf(l)) * 0.69314718055994531f;
-}
-
-constexpr int kMaxWorkgroups = 512;
-constexpr size_t kWorkspace = (size_t)2 * kMaxWorkgroups * 64 * (TKV_D + 2) * sizeof(float);
+// Room for the parts: two of every wave.
+constexpr size_t kPartRows = (size_t)2 * kWaves * kMaxUnits * 64;
+static_assert(48 * workgroups_each<16, 3>() <= 64 && 32 * workgroups_each<4, 2>() <= 64 && 16 * workgroups_each<4, 1>() <= 64, "workspace");
+static_assert(4 * kWaves * kMaxUnits * workgroups_each<4, 1>() <= TKV_PAGED_COUNTERS, "workspace");
+constexpr size_t kWorkspace = kPartRows * (TKV_D + 2) * sizeof(float) + TKV_PAGED_COUNTERS;
 
 template <typename T, int BITS, int NT>
 int32_t launch_attn(PagedParams& p, int units, hipStream_t s) {
-  constexpr int lds = lds_bytes<BITS, NT>(), each = lds <= 80 * 1024 && BITS == 4 && NT < 4 ? 2 : 1;
-  static_assert(lds <= 160 * 1024, "LDS of one compute unit");
+  constexpr int lds = lds_bytes<T, BITS, NT>();
+  static_assert(lds * workgroups_each<BITS, NT>() <= 160 * 1024, "LDS of one compute unit");
   static const bool lds_ok = hipFuncSetAttribute(reinterpret_cast<const void*>(&paged_attn_kernel<T, BITS, NT>),
                                                  hipFuncAttributeMaxDynamicSharedMemorySize, lds) == hipSuccess;
   if (!lds_ok) return TKV_E_HIP;
-  p.workgroups = std::min(kMaxWorkgroups, units * each);
-  p.ml = p.parts + (size_t)2 * kMaxWorkgroups * 64 * TKV_D;
+  p.workgroups = std::min(kMaxUnits, units) * workgroups_each<BITS, NT>();
   TKV_LAUNCH((paged_attn_kernel<T, BITS, NT>), dim3((uint32_t)p.workgroups), 64 * kWaves, lds, s, p);
-  if (p.workgroups > 1)
-    TKV_LAUNCH((paged_merge_kernel<T, BITS, NT>), dim3((uint32_t)p.workgroups - 1, 4 * NT), 256, 0, s, p);
   return TKV_OK;
 }
 
 template <typename T, int BITS>
 int32_t launch_rows(PagedParams& p, int64_t rows, int units, hipStream_t s) {
-  if (rows <= 16) return launch_attn<T, BITS, 1>(p, units, s);
-  if (rows <= 32) return launch_attn<T, BITS, 2>(p, units, s);
-  return launch_attn<T, BITS, 4>(p, units, s);
+  // Tiles of 16, 32 or (16 bits) 48 rows: what a wave's registers have room for, as few tiles as go, as small as go.
+  constexpr int kMost = BITS == 16 ? 3 : 2;
+  const int64_t sixteens = (rows + 15) / 16, tiles = (sixteens + kMost - 1) / kMost, each = (sixteens + tiles - 1) / tiles;
+  if (each == 1) return launch_attn<T, BITS, 1>(p, units, s);
+  if constexpr (BITS == 16)
+    if (each == 3) return launch_attn<T, BITS, 3>(p, units, s);
+  return launch_attn<T, BITS, 2>(p, units, s);
 }
 
 // Whether rows of 128 elements at p s[0] + h s[1] + t s[2] do not overlap, each axis beyond all that smaller strides span.
@@ -714,18 +961,19 @@ extern "C" int32_t tkv_paged_attn_sizes(const tkv_paged_desc* d, size_t* workspa
 
 extern "C" int32_t tkv_paged_attn(const tkv_paged_desc* d, const void* k_pages, const void* v_pages, int32_t batch, int32_t n_tokens,
                                   int32_t max_q_len, const void* q, void* out, float* lse, const int32_t* page_table,
-                                  int32_t pages_each, const int32_t* k_lens, const int32_t* q_starts, float sm_scale, void* workspace,
-                                  size_t workspace_bytes, void* stream) {
+                                  int32_t pages_each, const int32_t* k_lens, const int32_t* q_starts, int32_t clear_rest, float sm_scale,
+                                  void* workspace, size_t workspace_bytes, void* stream) {
   int32_t st = tkv::check_paged_desc(d);
   if (st != TKV_OK) return st;
   if (batch < 0 || n_tokens < 0 || max_q_len <= 0 || pages_each < 0 || !workspace) return TKV_E_INVAL;
+  if (clear_rest != 0 && clear_rest != 1) return TKV_E_INVAL;
   const float scale2 = sm_scale * 1.4426950408889634f;
   if (!(sm_scale > 0.f) || !(scale2 <= 3.402823466e38f)) return TKV_E_INVAL;
   if (!q_starts && (n_tokens != batch || max_q_len != 1)) return TKV_E_INVAL;
   if ((int64_t)pages_each * d->page_size > 0x7FFFFFFF) return TKV_E_UNSUPPORTED;
   if (workspace_bytes < kWorkspace) return TKV_E_WORKSPACE;
-  if (n_tokens == 0 || batch == 0) return TKV_OK;
-  if (!q || !out || !k_lens || (pages_each && !page_table)) return TKV_E_INVAL;
+  if (n_tokens == 0 || (batch == 0 && !(q_starts && clear_rest))) return TKV_OK;
+  if (!q || !out || (batch && !k_lens) || (batch && pages_each && !page_table)) return TKV_E_INVAL;
   for (const void* x : {q, (const void*)out, (const void*)workspace})
     if (((uintptr_t)x & 15) != 0) return TKV_E_INVAL;
   for (const void* x : {(const void*)lse, (const void*)page_table, (const void*)k_lens, (const void*)q_starts})
@@ -740,6 +988,9 @@ extern "C" int32_t tkv_paged_attn(const tkv_paged_desc* d, const void* k_pages, 
   p.group = d->n_q_heads / d->n_kv_heads;
   p.scale2 = scale2;
   p.parts = (float*)workspace;
+  p.ml = p.parts + kPartRows * TKV_D;
+  p.arrivals = (uint32_t*)(p.ml + kPartRows * 2);
+  p.clear_rest = q_starts && clear_rest;
   // (numbers of tiles are 32 bits: tiles of 16 rows and 32 keys, the smallest)
   const int64_t row_tiles = (int64_t)n_tokens * p.group / 16 + batch, key_tiles = (((int64_t)pages_each * d->page_size) >> 5) + 1;
   if (row_tiles * d->n_kv_heads >= ((int64_t)1 << 31) || row_tiles * d->n_kv_heads * key_tiles >= ((int64_t)1 << 31)) return TKV_E_UNSUPPORTED;

@@ -136,7 +136,7 @@ def lib() -> C.CDLL:
         L.tkv_paged_append.argtypes = [C.POINTER(PagedDesc), C.POINTER(RopeDesc), i32] + [vp] * 6 + [i32] + [vp] * 8
         L.tkv_paged_gather.argtypes = [C.POINTER(PagedDesc), vp, vp, i32] + [vp] * 4
         L.tkv_paged_attn_sizes.argtypes = [C.POINTER(PagedDesc), C.POINTER(sz)]
-        L.tkv_paged_attn.argtypes = [C.POINTER(PagedDesc), vp, vp, i32, i32, i32, vp, vp, vp, vp, i32, vp, vp, C.c_float, vp, sz, vp]
+        L.tkv_paged_attn.argtypes = [C.POINTER(PagedDesc), vp, vp, i32, i32, i32, vp, vp, vp, vp, i32, vp, vp, i32, C.c_float, vp, sz, vp]
         L.tkv_prompt_attn_sizes.argtypes = [C.POINTER(PromptDesc), C.POINTER(sz)]
         L.tkv_prompt_attn.argtypes = [C.POINTER(PromptDesc)] + [vp] * 9 + [C.c_float, vp, sz, vp]
         L.tkv_quant_attn_decode_shared_sizes.argtypes = [C.POINTER(QuantDesc), C.POINTER(QuantDesc), C.POINTER(sz)]
@@ -201,14 +201,22 @@ def _new(shape, dtype, device, stream, fill=None) -> torch.Tensor:
     return torch.empty(shape, dtype=dtype, device=device) if fill is None else torch.full(shape, fill, dtype=dtype, device=device)
 
 
+def _like(x: torch.Tensor, dtype, stream) -> torch.Tensor:
+    """A new contiguous output of x's shape.  (empty_like spares a microsecond of torch.empty's two.)"""
+    if stream is not None:
+        return _new(x.shape, dtype, x.device, stream)
+    return torch.empty_like(x, dtype=dtype, memory_format=torch.contiguous_format)
+
+
 class _Workspaces:
     """The workspaces of an object's calls: one for every stream, whose calls follow each other, and one of its own for every call made
     while the current stream is captured into a graph (it stays in the graph's memory pool), as graphs may be replayed beside each
     other and beside eager calls.  Threads hold `lock` while their call's launches go out, so that none of another thread's, with
     the same workspace, comes in between."""
 
-    def __init__(self, n_bytes: int, device: torch.device, at_once: bool = True):
-        self._bytes, self._device, self._of = n_bytes, device, {}
+    def __init__(self, n_bytes: int, device: torch.device, at_once: bool = True, zeros: int = 0):
+        """zeros: bytes at the end that are zero-filled when a workspace is made."""
+        self._bytes, self._device, self._of, self._zeros = n_bytes, device, {}, zeros
         self.lock = threading.Lock()
         if at_once:
             with torch.cuda.device(device):
@@ -219,6 +227,9 @@ class _Workspaces:
         w = None if captured else self._of.get(handle)
         if w is None:
             w = _new(self._bytes, torch.uint8, self._device, stream)
+            if self._zeros:
+                with torch.cuda.stream(stream if hasattr(stream, "cuda_stream") else torch.cuda.ExternalStream(handle, device=self._device)):
+                    w[-self._zeros:].zero_()
             if not captured:
                 self._of[handle] = w
         return w
@@ -699,7 +710,7 @@ def qk_norm_rope(q: torch.Tensor, k: torch.Tensor, positions: torch.Tensor | Non
     None) in out_dtype (default: the inputs').  With axis_of (bytes or small numbers, an axis for every frequency; see rope_axes) positions
     are int32 [axes, T]: tkv_qk_norm_rope_axes."""
     shape_q, shape_k = q.shape, k.shape
-    dt, dev, at = q.dtype, q.device, q.get_device()
+    dt, at = q.dtype, q.get_device()
     _on_current(q, stream)
     if axis_of is not None:
         axis_of = bytes(axis_of)
@@ -709,11 +720,11 @@ def qk_norm_rope(q: torch.Tensor, k: torch.Tensor, positions: torch.Tensor | Non
     for o, shape in ((q_out, shape_q), (k_out, shape_k), (v_out, shape_k if v is not None else None)):
         assert o is None or (o.dtype == out_dtype and o.shape == shape and o.is_contiguous() and o.get_device() == at)
     if q_out is None:
-        q_out = _new(shape_q, out_dtype, dev, stream)
+        q_out = _like(q, out_dtype, stream)
     if k_out is None:
-        k_out = _new(shape_k, out_dtype, dev, stream)
+        k_out = _like(k, out_dtype, stream)
     if v_out is None and v is not None:
-        v_out = _new(shape_k, out_dtype, dev, stream)
+        v_out = _like(v, out_dtype, stream)
     pos, freq = (_ptr(positions), _ptr(inv_freq)) if desc.rotary_dim else (0, 0)
     outs = q_out.data_ptr(), k_out.data_ptr(), _ptr(v_out), _stream(stream)
     if axis_of is None:
@@ -762,7 +773,7 @@ class PagedCache:
         self.device, self._at = k_pages.device, k_pages.get_device()
         self._pages = k_pages.data_ptr(), v_pages.data_ptr()
         self._rows = (n_q_heads, head_dim), (n_kv_heads, head_dim)
-        self._workspaces = _Workspaces(self.workspace_bytes, torch.device("cuda", self._at), at_once=False)  # (a cache that is only filled needs none)
+        self._workspaces = _Workspaces(self.workspace_bytes, torch.device("cuda", self._at), at_once=False, zeros=12288)  # (a cache that is only filled needs none)
 
     def _slots(self, slots, t):
         assert slots.dtype == torch.int32 and slots.shape == (t,) and slots.is_contiguous() and slots.get_device() == self._at
@@ -785,7 +796,7 @@ class PagedCache:
         if q is None:
             assert q_out is None
         elif q_out is None:
-            q_out = _new(q.shape, self.dtype, q.device, stream)
+            q_out = _like(q, self.dtype, stream)
         for o, x in ((q_out, q), (k_out, k)):
             assert o is None or (o.dtype == self.dtype and o.shape == x.shape and o.is_contiguous() and o.get_device() == at)
         pos, freq = (_ptr(positions), _ptr(inv_freq)) if desc.rotary_dim else (0, 0)
@@ -827,12 +838,15 @@ class PagedCache:
             assert t == b
         else:
             assert q_starts.dtype == torch.int32 and q_starts.shape == (b + 1,) and q_starts.is_contiguous() and q_starts.get_device() == at
+        new_lse = lse is True
+        clear = q_starts is not None and out is None and (new_lse or not isinstance(lse, torch.Tensor))  # (by the call itself)
+        fill = q_starts is not None and not clear
         if out is None:
-            out = _new(q.shape, q.dtype, q.device, stream, None if q_starts is None else 0.0)
+            out = _new(q.shape, q.dtype, q.device, stream, 0.0) if fill else _like(q, q.dtype, stream)
         else:
             assert out.dtype == q.dtype and out.shape == q.shape and out.is_contiguous() and out.get_device() == at
-        if lse is True:
-            lse = _new((t, d.n_q_heads), torch.float32, q.device, stream, None if q_starts is None else -float("inf"))
+        if new_lse:
+            lse = _new((t, d.n_q_heads), torch.float32, q.device, stream, -float("inf") if fill else None)
         elif lse is False or lse is None:
             lse = None
         else:
@@ -841,7 +855,7 @@ class PagedCache:
         with self._workspaces.lock:
             workspace = self._workspaces.of(handle, stream)
             status = lib().tkv_paged_attn(C.byref(d), *self._pages, b, t, int(max_q_len), q.data_ptr(), out.data_ptr(), _ptr(lse),
-                                          page_table.data_ptr(), each, k_lens.data_ptr(), _ptr(q_starts), float(sm_scale),
+                                          page_table.data_ptr(), each, k_lens.data_ptr(), _ptr(q_starts), clear, float(sm_scale),
                                           workspace.data_ptr(), self.workspace_bytes, handle)
         _check(status, "tkv_paged_attn")
         return out if lse is None else (out, lse)

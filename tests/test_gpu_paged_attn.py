@@ -159,8 +159,38 @@ def test_rows_of_no_sequence_are_left():
     torch.cuda.synchronize()
     assert got[0] is out and torch.equal(out[2:7], want)
     assert (out[:2] == 7).all() and (out[7:] == 7).all() and (lse[:2] == 5).all() and (lse[7:] == 5).all() and lse[2:7].isfinite().all()
-    new = cache.attend(wide, SM, table, lens, q_starts=starts, max_q_len=3)
-    assert torch.equal(new[2:7], want) and not new[:2].any() and not new[7:].any()
+    for given in (dict(), dict(lse=True), dict(lse=torch.full((9, 4), 5.0, device="cuda")), dict(out=torch.full_like(wide, 7.0), lse=True)):
+        junk = torch.full((1 << 20,), float("nan"), device="cuda")     # (what a new tensor's memory may hold)
+        del junk
+        new = cache.attend(wide, SM, table, lens, q_starts=starts, max_q_len=3, **given)
+        new, new_lse = new if isinstance(new, tuple) else (new, None)
+        torch.cuda.synchronize()
+        rest = torch.cat((new[:2], new[7:]))
+        assert torch.equal(new[2:7], want) and (rest == (7 if "out" in given else 0)).all()
+        if new_lse is not None:
+            rest = torch.cat((new_lse[:2], new_lse[7:]))
+            assert torch.equal(new_lse[2:7], lse[2:7])
+            assert (rest == 5).all() if isinstance(given["lse"], torch.Tensor) else torch.isneginf(rest).all()
+
+
+def test_rows_of_no_sequence_and_of_none_at_all():
+    """Every workgroup clears its share: more rows than workgroups, around one short sequence, and no sequences."""
+    cache = tkv.PagedCache(n_q_heads=4, n_kv_heads=2, n_pages=2)
+    q = torch.randn(1500, 4, 128, device="cuda").half()
+    starts = torch.tensor([700, 701], device="cuda", dtype=torch.int32)
+    table, lens = torch.zeros(1, 1, device="cuda", dtype=torch.int32), torch.tensor([5], device="cuda", dtype=torch.int32)
+    cache.v_pages[0, :, :5] = 3
+    junk = torch.full((1 << 22,), float("nan"), device="cuda")
+    del junk
+    out, lse = cache.attend(q, SM, table, lens, q_starts=starts, lse=True)
+    torch.cuda.synchronize()
+    assert (out[700] == 3).all() and not out[:700].any() and not out[701:].any()
+    assert lse[700].isfinite().all() and torch.isneginf(lse[:700]).all() and torch.isneginf(lse[701:]).all()
+    out, lse = cache.attend(q[:3], SM, table[:0], lens[:0], q_starts=starts[:1] * 0, lse=True)
+    torch.cuda.synchronize()
+    assert not out.any() and torch.isneginf(lse).all()
+    out = cache.attend(q[:0], SM, table[:0], lens[:0])
+    assert tuple(out.shape) == (0, 4, 128)
 
 
 @BOTH

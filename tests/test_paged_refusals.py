@@ -114,7 +114,7 @@ def test_gather(L, kw, status):
 
 
 def _attn(L, desc=None, ptr=None, batch=3, n=3, most=1, each=7, scale=0.1, ws=1 << 40):
-    args = dict(k_pages=A, v_pages=A, batch=batch, n=n, most=most, q=A, out=A, lse=A, table=A, each=each, k_lens=A, q_starts=0, scale=scale,
+    args = dict(k_pages=A, v_pages=A, batch=batch, n=n, most=most, q=A, out=A, lse=A, table=A, each=each, k_lens=A, q_starts=0, clear=0, scale=scale,
                 workspace=A, ws=ws)
     args.update(ptr or {})
     return L.tkv_paged_attn(C.byref(_paged(**(desc or {}))), *args.values(), None)
@@ -127,7 +127,7 @@ def _attn(L, desc=None, ptr=None, batch=3, n=3, most=1, each=7, scale=0.1, ws=1 
     (dict(ptr=dict(q=0)), -1), (dict(ptr=dict(q=A + 8)), -1), (dict(ptr=dict(out=0)), -1), (dict(ptr=dict(out=A + 2)), -1),
     (dict(ptr=dict(lse=A + 2)), -1), (dict(ptr=dict(table=0)), -1), (dict(ptr=dict(table=A + 1)), -1), (dict(ptr=dict(k_lens=0)), -1),
     (dict(ptr=dict(k_lens=A + 2)), -1), (dict(ptr=dict(q_starts=A + 2)), -1), (dict(ptr=dict(k_pages=0)), -1),
-    (dict(ptr=dict(v_pages=A + 8)), -1), (dict(batch=0, n=0), 0), (dict(batch=0, n=5, ptr=dict(q_starts=A)), 0),
+    (dict(ptr=dict(v_pages=A + 8)), -1), (dict(ptr=dict(clear=2)), -1), (dict(batch=0, n=0), 0), (dict(batch=0, n=5, ptr=dict(q_starts=A)), 0),
     (dict(n=0, ptr=dict(q_starts=A)), 0),
 ])
 def test_attn(L, kw, status):
@@ -139,7 +139,7 @@ def test_null_descriptors(L):
     assert L.tkv_paged_append(None, C.byref(_rope()), 1, *([A] * 5), None, 1, *([A] * 7), None) == -1
     assert L.tkv_paged_append(C.byref(_paged()), None, 1, *([A] * 5), None, 1, *([A] * 7), None) == -1
     assert L.tkv_paged_gather(None, A, A, 1, A, A, A, None) == -1
-    assert L.tkv_paged_attn(None, A, A, 1, 1, 1, A, A, A, A, 1, A, None, 0.1, A, 1 << 40, None) == -1
+    assert L.tkv_paged_attn(None, A, A, 1, 1, 1, A, A, A, A, 1, A, None, 0, 0.1, A, 1 << 40, None) == -1
 
 
 def test_axes_of_sections():
