@@ -613,7 +613,8 @@ int32_t tkv_paged_attn_sizes(const tkv_paged_desc* desc, size_t* workspace_bytes
  * out = softmax(sm_scale q.k) v; a token that sees no key yields zeros, and -inf in lse.
  * q, out [n_tokens][Hq][128] contiguous; lse float32 [n_tokens][Hq] (natural logarithm of the sum of exponentials) or NULL.  Rows of out and
  * lse that belong to no sequence (in front of the first, behind the last) are left as they were, or with clear_rest = 1 get zeros and
- * -inf.  max_q_len: the most queries that a sequence has, as the host knows it.
+ * -inf.  max_q_len: the most queries that a sequence has, as the host knows it; q_starts that say more
+ * count as that many.  batch * (tiles of 16 rows of max_q_len * Hq / Hkv) * Hkv * (pages_each * page_size / 32 + 1) < 2^31.
  * Keys behind a sequence's last are never used, whatever their slots hold.  A page number outside the cache stands for rows of zeros; k_lens
  * beyond pages_each * page_size, or below 0, count as that, or as 0.
  * Products in desc->dtype with float32 sums (4 bits: of what the codes stand for, exactly); softmax statistics in float32.

@@ -89,7 +89,7 @@ struct PagedParams {
   float* parts;             // [2 per wave][rows of a tile][128] weighted sums
   float* ml;                // [2 per wave][rows of a tile][2] (reference, sum)
   uint32_t* arrivals;       // [wave] parts, of the item whose first cut lies behind its range, that have come in
-  int32_t n_tokens, batch, hq, group, pages_each;
+  int32_t n_tokens, batch, max_q_len, hq, group, pages_each;
   int32_t workgroups;
   int32_t clear_rest;  // rows of no sequence get zeros
   float scale2;        // sm_scale * log2(e)
@@ -145,7 +145,7 @@ struct Walk {
       q_len = 1;
       if (starts) {
         q_start = min(max(starts[b], 0), p->n_tokens);
-        q_len = max(0, min(starts[b + 1], p->n_tokens) - q_start);
+        q_len = max(0, min(min(starts[b + 1], p->n_tokens) - q_start, p->max_q_len));
       }
     }
     count = (uint32_t)(key_tiles(k_len) * row_tiles(q_len)) * (uint32_t)p->pages.hkv;  // (no rows: 0)
@@ -167,14 +167,12 @@ struct Walk {
     if (chunk != 0) load(0, 0);
     return t;
   }
-  // The place of tile number `at` (not before the chunk at hand); sq.index -1 where there is none.
+  // The place of tile number `at`, below total() and not before the chunk at hand.
   __device__ Place find(uint32_t at) {
     while (at >= all && chunk + 64 < batch) load(chunk + 64, all);
     const uint64_t here = __builtin_amdgcn_ballot_w64(first <= at && at < first + count);
+    const int l = here ? __builtin_ctzll(here) : 0;
     Place x;
-    x.sq.index = -1;
-    if (here == 0) return x;
-    const int l = __builtin_ctzll(here);
     x.sq.index = chunk + l;
     x.sq.k_len = __builtin_amdgcn_readlane(k_len, l);
     x.sq.q_start = __builtin_amdgcn_readlane(q_start, l);
@@ -522,12 +520,18 @@ struct Tiles4 {
 template <typename T, int BITS, int NT>
 using Tiles = std::conditional_t<BITS == 16, Tiles16<T, NT>, Tiles4<T, NT>>;
 
+// What is left to join by a workgroup whose waves work alone: of each wave, the items at its range's two ends, if it came last.
+struct Won {
+  int32_t count;
+  Place at[2];
+};
+
 // Workgroups of a compute unit: what registers and LDS have room for.  LDS: the waves' rings or areas, and the waves' results where they join.
 template <int BITS, int NT>
 constexpr int workgroups_each() { return BITS == 16 ? 1 : 2; }
 template <typename T, int BITS, int NT>
 constexpr int lds_bytes() {
-  return std::max(kWaves * Tiles<T, BITS, NT>::kBytes, kWaves * 16 * (kRowFloats + 2) * 4 + 16);
+  return std::max(kWaves * Tiles<T, BITS, NT>::kBytes, kWaves * 16 * (kRowFloats + 2) * 4 + 16) + (int)sizeof(Won) * kWaves;
 }
 
 // Zeros, and -inf, for rows in front of the first sequence and behind the last.
@@ -603,7 +607,7 @@ __device__ inline float log_sum(float ref, float sum) {
 }
 
 // A wave joins an item's parts for some of its rows: row0, row0 + step, ...  A row's parts are shared out over the wave's four sixteens of
-// lanes, a lane has eight channels.  Four loads are on their way at once, of four rows where there are no more than four parts.
+// lanes, a lane has eight channels.  Four times four parts are on their way at once, of four rows where there are no more than four.
 // What is added up in which order depends on the number of parts alone: the same bits, whoever comes last.
 template <typename T, int ROWS>
 __device__ inline void join_rows(Args p, const Place& x, const Parts& parts, int row0, int step) {
@@ -683,7 +687,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void paged_attn_kernel(PagedParams)
   Place x = walk.find(begin < end ? begin : (uint32_t)group_begin);
   // Whether the workgroup's whole range lies in one item (all its waves find the same): then they take its tiles in turn, and join before
   // they hand on.
-  const bool together = x.sq.index >= 0 && x.start <= (uint32_t)group_begin &&
+  const bool together = x.start <= (uint32_t)group_begin &&
                         (uint64_t)x.start + (uint32_t)x.sq.key_tiles >= min((uint64_t)total, group_begin + (uint64_t)kWaves * pw);
 
   Rows<NT> r;
@@ -722,36 +726,35 @@ __global__ __launch_bounds__(64 * kWaves, 2) void paged_attn_kernel(PagedParams)
     begin = (uint32_t)min((uint64_t)total, group_begin + (uint64_t)wave);
     end = (uint32_t)min((uint64_t)total, group_begin + (uint64_t)kWaves * pw);
   }
-  if (x.sq.index < 0 || (!together && begin >= end)) return;  // (the first not with ascending q_starts)
+  Won* const won = (Won*)(lds + lds_bytes<T, BITS, NT>()) - kWaves;
+  int wins = 0;
   Tile tiles((lds_char*)lds + wave * Tile::kBytes);
   Plan<Tile::kPer> plan;
   plan.log_step = together ? 2 : 0;
   static_assert(kWaves == 4, "log_step");
   const uint32_t step = 1u << plan.log_step;
-  open(x);
+  if (begin < end || together) open(x);
   if (begin < end) {
     plan.make(walk, begin, end);
     tiles.begin(plan, begin);
   }
-  reset(x);
-  for (uint32_t at = begin;;) {
+  if (begin < end || together) reset(x);
+  for (uint32_t at = begin; begin < end || together;) {
     const uint32_t stop = min(end, x.start + (uint32_t)x.sq.key_tiles);
     const bool begins = at == begin;
     for (; at < stop; at += step)
       tiles.work(plan, at + step, at + step < end, [&] { if (__builtin_expect(!plan.has(at + step), 0)) plan.make(walk, at + step, end); },
                  Tile::kKeys * (int)(at - x.start), qf, r);
     const Place done = x;
-    bool last = together || at >= end;
+    const bool last = together || at >= end;
     if (!last) {  // the next item's rows are on their way while this one's results leave
       x = walk.find(at);
-      last = x.sq.index < 0;
-      if (!last) open(x);
+      open(x);
     }
     const Args p = arguments();
     const Parts parts(done, pw, total);
     const PartStore<kRows> store(p);
     const int rows = done.sq.q_len * walk.group;
-    bool joins = false;
     if (!together) {
       const int slot = 2 * (kWaves * (int)blockIdx.x + wave) + (begins ? 0 : 1);
 #pragma unroll
@@ -776,7 +779,10 @@ __global__ __launch_bounds__(64 * kWaves, 2) void paged_attn_kernel(PagedParams)
         asm volatile("s_waitcnt vmcnt(0)" ::: "memory");  // the part is in memory before the count goes up
         uint32_t before = 0;
         if (lane == 0) before = atomicAdd(p->arrivals + parts.w0, 1u);
-        joins = (uint32_t)__builtin_amdgcn_readfirstlane((int)before) == (uint32_t)parts.count - 1u;
+        if ((uint32_t)__builtin_amdgcn_readfirstlane((int)before) == (uint32_t)parts.count - 1u) {
+          if (lane == 0) won[wave].at[wins] = done;
+          ++wins;
+        }
       }
     } else {
       // the waves join, sixteen rows at a time: everyone's results into LDS, then sixteen threads a row
@@ -822,15 +828,33 @@ __global__ __launch_bounds__(64 * kWaves, 2) void paged_attn_kernel(PagedParams)
         uint32_t* const flag = (uint32_t*)(ml_s + 2 * kWaves * 16);
         if (threadIdx.x == 0) *flag = atomicAdd(p->arrivals + parts.w0, 1u);
         __syncthreads();
-        joins = *flag == (uint32_t)parts.count - 1u;
+        wins = *flag == (uint32_t)parts.count - 1u ? 1 : 0;
       }
     }
-    if (joins) {
-      if (lane == 0) __hip_atomic_store(p->arrivals + parts.w0, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-      join_rows<T, kRows>(p, done, parts, together ? wave : 0, together ? kWaves : 1);
-    }
-    if (last) return;
+    if (last) break;
     reset(x);
+  }
+  uint32_t left = (uint32_t)__builtin_amdgcn_readfirstlane(wins);
+  if (!together) {  // all waves take part in what any of them has won: bit 2 w + i
+    if (lane == 0) won[wave].count = wins;
+    __syncthreads();
+    left = (uint32_t)__builtin_amdgcn_ballot_w64(lane < 2 * kWaves && lane % 2 < won[lane / 2 % kWaves].count);
+  }
+  for (; left != 0; left &= left - 1) {
+    Place at = x;
+    static_assert(sizeof(Place) % 4 == 0, "words");
+    const int i = __builtin_ctz(left);
+    if (!together) {
+#pragma unroll
+      for (int k = 0; k < (int)sizeof(Place) / 4; ++k) ((int32_t*)&at)[k] = __builtin_amdgcn_readfirstlane(((const int32_t*)&won[i / 2].at[i % 2])[k]);
+    }
+    const Args p = arguments();
+    const Parts parts(at, pw, total);
+    if (threadIdx.x == 0) __hip_atomic_store(p->arrivals + parts.w0, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    // (few rows in few parts are one wave's)
+    const bool alone = !together && parts.count <= 4 && at.sq.q_len * walk.group <= 4;
+    if (alone && i / 2 != wave) continue;
+    join_rows<T, kRows>(p, at, parts, alone ? 0 : wave, alone ? 1 : kWaves);
   }
 }
 
@@ -983,7 +1007,7 @@ extern "C" int32_t tkv_paged_attn(const tkv_paged_desc* d, const void* k_pages, 
   if (st != TKV_OK) return st;
   p.q = q; p.out = out; p.lse = lse;
   p.table = page_table; p.k_lens = k_lens; p.q_starts = q_starts;
-  p.n_tokens = n_tokens; p.batch = batch; p.pages_each = pages_each;
+  p.n_tokens = n_tokens; p.batch = batch; p.max_q_len = max_q_len; p.pages_each = pages_each;
   p.hq = d->n_q_heads;
   p.group = d->n_q_heads / d->n_kv_heads;
   p.scale2 = scale2;
@@ -991,10 +1015,11 @@ extern "C" int32_t tkv_paged_attn(const tkv_paged_desc* d, const void* k_pages, 
   p.ml = p.parts + kPartRows * TKV_D;
   p.arrivals = (uint32_t*)(p.ml + kPartRows * 2);
   p.clear_rest = q_starts && clear_rest;
-  // (numbers of tiles are 32 bits: tiles of 16 rows and 32 keys, the smallest)
-  const int64_t row_tiles = (int64_t)n_tokens * p.group / 16 + batch, key_tiles = (((int64_t)pages_each * d->page_size) >> 5) + 1;
+  // Numbers of tiles are 32 bits, whatever the device's arrays hold: tiles of 16 rows and 32 keys, the smallest.
+  max_q_len = std::min(max_q_len, n_tokens);
+  if ((int64_t)max_q_len * p.group > (1 << 24)) return TKV_E_UNSUPPORTED;
+  const int64_t row_tiles = (int64_t)batch * (((int64_t)max_q_len * p.group + 15) / 16), key_tiles = (((int64_t)pages_each * d->page_size) >> 5) + 1;
   if (row_tiles * d->n_kv_heads >= ((int64_t)1 << 31) || row_tiles * d->n_kv_heads * key_tiles >= ((int64_t)1 << 31)) return TKV_E_UNSUPPORTED;
-  if ((int64_t)n_tokens * p.group > (1 << 30)) return TKV_E_UNSUPPORTED;
   const int64_t rows = (int64_t)max_q_len * p.group;
   const auto s = (hipStream_t)stream;
   const int units = tkv::stream_compute_units(s);

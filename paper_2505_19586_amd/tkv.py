@@ -822,10 +822,10 @@ class PagedCache:
         return outs[0], outs[1]
 
     def attend(self, q: torch.Tensor, sm_scale: float, page_table: torch.Tensor, k_lens: torch.Tensor, *,
-               q_starts: torch.Tensor | None = None, max_q_len: int = 1, out: torch.Tensor | None = None,
+               q_starts: torch.Tensor | None = None, max_q_len: int | None = None, out: torch.Tensor | None = None,
                lse: bool | torch.Tensor = False, stream=None):
         """tkv_paged_attn: q [T, Hq, 128]; page_table int32 [B, pages], k_lens int32 [B]: each sequence's pages and tokens, the queries'
-        own among them; q_starts int32 [B + 1]: where each sequence's rows of q begin, max_q_len of them at most (None: row b is
+        own among them; q_starts int32 [B + 1]: where each sequence's rows of q begin, max_q_len of them at most (both None: row b is
         sequence b's only one).  Returns out [T, Hq, 128], or (out, lse [T, Hq]) where lse is True or a float32 tensor.  Rows of no
         sequence are left as they were (a new out has zeros there)."""
         t, at, d = q.shape[0], self._at, self.desc
@@ -835,8 +835,10 @@ class PagedCache:
         assert page_table.dtype == torch.int32 and page_table.is_contiguous() and page_table.get_device() == at
         assert k_lens.dtype == torch.int32 and k_lens.shape == (b,) and k_lens.is_contiguous() and k_lens.get_device() == at
         if q_starts is None:
-            assert t == b
+            assert t == b and max_q_len in (None, 1)
+            max_q_len = 1
         else:
+            assert max_q_len is not None, "max_q_len: the most queries of a sequence"
             assert q_starts.dtype == torch.int32 and q_starts.shape == (b + 1,) and q_starts.is_contiguous() and q_starts.get_device() == at
         new_lse = lse is True
         clear = q_starts is not None and out is None and (new_lse or not isinstance(lse, torch.Tensor))  # (by the call itself)

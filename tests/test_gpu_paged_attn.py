@@ -144,9 +144,24 @@ def test_long_single_sequence(bits):
 
 
 def test_a_bound_on_queries_that_is_not_reached_or_too_small():
-    """max_q_len is what the host knows: the result is right whatever it says."""
-    for most in (1, 2, 9, 1000):
+    """max_q_len is what the host knows: any bound does; more queries than it says count as that many."""
+    for most in (40, 41, 100, 1 << 30):
         _run([3, 1, 40], [50, 77, 130], 8, 2, 32, 16, seed=7, most=most)
+    cache, q, table, lens, _ = _run([3, 1, 40], [50, 77, 130], 8, 2, 32, 16, seed=7)
+    got = cache.attend(q, SM, table, lens, q_starts=torch.tensor([0, 3, 4, 44], device="cuda", dtype=torch.int32), max_q_len=2)
+    want = cache.attend(torch.cat((q[:2], q[3:6])), SM, table, lens, q_starts=torch.tensor([0, 2, 3, 5], device="cuda", dtype=torch.int32), max_q_len=2)
+    torch.cuda.synchronize()
+    assert torch.equal(torch.cat((got[:2], got[3:6])), want)
+
+
+def test_starts_that_do_not_ascend_end():
+    """Invalid, but nothing out of bounds is touched and every wave ends: rows of sequences that are sound come out."""
+    cache, q, table, lens, want = _run([1] * 5, [50, 77, 130, 9, 64], 8, 2, 32, 16, seed=7)
+    for starts in ([0, 1, 2, 1, 4, 5], [-7, 1, 2, 3, 4, 5], [0, 1, 2, 3, 4, 1 << 30], [5, 4, 3, 2, 1, 0]):
+        got = cache.attend(q, SM, table, lens, q_starts=torch.tensor(starts, device="cuda", dtype=torch.int32), max_q_len=3)
+        torch.cuda.synchronize()
+        if starts[1:4] == [1, 2, 3]:
+            assert torch.equal(got[1], want[1])
 
 
 def test_rows_of_no_sequence_are_left():
@@ -182,11 +197,11 @@ def test_rows_of_no_sequence_and_of_none_at_all():
     cache.v_pages[0, :, :5] = 3
     junk = torch.full((1 << 22,), float("nan"), device="cuda")
     del junk
-    out, lse = cache.attend(q, SM, table, lens, q_starts=starts, lse=True)
+    out, lse = cache.attend(q, SM, table, lens, q_starts=starts, max_q_len=1, lse=True)
     torch.cuda.synchronize()
     assert (out[700] == 3).all() and not out[:700].any() and not out[701:].any()
     assert lse[700].isfinite().all() and torch.isneginf(lse[:700]).all() and torch.isneginf(lse[701:]).all()
-    out, lse = cache.attend(q[:3], SM, table[:0], lens[:0], q_starts=starts[:1] * 0, lse=True)
+    out, lse = cache.attend(q[:3], SM, table[:0], lens[:0], q_starts=starts[:1] * 0, max_q_len=1, lse=True)
     torch.cuda.synchronize()
     assert not out.any() and torch.isneginf(lse).all()
     out = cache.attend(q[:0], SM, table[:0], lens[:0])
