@@ -606,14 +606,14 @@ __device__ inline float log_sum(float ref, float sum) {
   return sum == 0.f ? -INFINITY : (ref - kShift + __builtin_amdgcn_logf(sum)) * 0.69314718055994531f;
 }
 
-// A wave joins an item's parts for some of its rows: row0, row0 + step, ...  A row's parts are shared out over the wave's four sixteens of
-// lanes, a lane has eight channels.  Four times four parts are on their way at once, of four rows where there are no more than four.
-// What is added up in which order depends on the number of parts alone: the same bits, whoever comes last.
-template <typename T, int ROWS>
+// A wave joins an item's parts for some of its rows, a lane eight channels: row0, row0 + step, ..., each row's parts shared out over the
+// wave's four sixteens of lanes (SHARES 4), or from each of these on four rows, a sixteen each (SHARES 1).  What is added up in which order
+// depends on SHARES and the number of parts alone: the same bits, whoever comes last.
+template <typename T, int ROWS, int SHARES>
 __device__ inline void join_rows(Args p, const Place& x, const Parts& parts, int row0, int step) {
-  constexpr int kAtOnce = 4;
-  const int lane = threadIdx.x % 64, share = lane / 16, c = 8 * (lane % 16);
-  const int rows = min(ROWS, x.sq.q_len * p->group - ROWS * x.tile), rounds = (parts.count + 3) / 4;
+  constexpr int kAtOnce = SHARES == 4 ? 4 : 8;  // loads on their way, in rounds of SHARES parts
+  const int lane = threadIdx.x % 64, share = SHARES == 4 ? lane / 16 : 0, sub = SHARES == 4 ? 0 : lane / 16, c = 8 * (lane % 16);
+  const int rows = min(ROWS, x.sq.q_len * p->group - ROWS * x.tile), rounds = (parts.count + SHARES - 1) / SHARES;
   const tkv::AgentBuf ob(p->parts, (uint32_t)(2 * kWaves * p->workgroups) * (ROWS * TKV_D * 4u));
   const tkv::AgentBuf mb(p->ml, (uint32_t)(2 * kWaves * p->workgroups) * (ROWS * 8u));
   float m = kNone, l = 0.f;
@@ -626,9 +626,9 @@ __device__ inline void join_rows(Args p, const Place& x, const Parts& parts, int
     int r = row, n = round;
 #pragma unroll
     for (int y = 0; y < kAtOnce; ++y) {
-      const int i = 4 * n + share;
-      const uint32_t at = (uint32_t)(parts.slot(min(i, parts.count - 1)) * ROWS + r);
-      const bool there = i < parts.count && r < rows;  // (absent ones are zeros)
+      const int i = SHARES * n + share;
+      const uint32_t at = (uint32_t)(parts.slot(min(i, parts.count - 1)) * ROWS + r + sub);
+      const bool there = i < parts.count && r + sub < rows;  // (absent ones are zeros)
       st[y] = mb.x2(there ? at * 8u : tkv::AgentBuf::kNone);
       lo[y] = ob.x4(there ? (at * TKV_D + c) * 4u : tkv::AgentBuf::kNone);
       hi[y] = ob.x4(there ? (at * TKV_D + c) * 4u + 16u : tkv::AgentBuf::kNone);
@@ -638,7 +638,7 @@ __device__ inline void join_rows(Args p, const Place& x, const Parts& parts, int
     for (int y = 0; y < kAtOnce; ++y) {
       if (row >= rows) break;
       const uint32_t ref_bits = st[y].x, sum_bits = st[y].y;
-      const float ref = 4 * round + share < parts.count ? __builtin_bit_cast(float, ref_bits) : kNone;
+      const float ref = SHARES * round + share < parts.count ? __builtin_bit_cast(float, ref_bits) : kNone;
       const float top = fmaxf(m, ref), shrink = __builtin_amdgcn_exp2f(m - top), w = __builtin_amdgcn_exp2f(ref - top);
       m = top;
       l = __builtin_fmaf(__builtin_bit_cast(float, sum_bits), w, l * shrink);
@@ -649,16 +649,20 @@ __device__ inline void join_rows(Args p, const Place& x, const Parts& parts, int
         acc[4 + k] = __builtin_fmaf(b[k], w, acc[4 + k] * shrink);
       }
       if (++round < rounds) continue;
-      // the row's last: the four sixteens together
-      auto max2 = [](float u, float v) { return fmaxf(u, v); };
-      auto add = [](float u, float v) { return u + v; };
-      const float all = tkv::over_rows(m, max2), mine = __builtin_amdgcn_exp2f(m - all), sum = tkv::over_rows(l * mine, add);
-      const float inv = sum == 0.f ? 0.f : 1.f / sum;  // (no key: zeros)
+      // the row's last
+      if constexpr (SHARES == 4) {
+        auto add = [](float u, float v) { return u + v; };
+        const float all = tkv::over_rows(m, [](float u, float v) { return fmaxf(u, v); }), mine = __builtin_amdgcn_exp2f(m - all);
+        m = all;
+        l = tkv::over_rows(l * mine, add);
 #pragma unroll
-      for (int k = 0; k < 8; ++k) acc[k] = tkv::over_rows(acc[k] * mine, add) * inv;
-      const int64_t to = row_out(p, x, ROWS * x.tile + row);
-      if (share == 0) *(uintx4*)((T*)p->out + to * TKV_D + c) = pack8<T>(acc);
-      if (p->lse && lane == 0) p->lse[to] = log_sum(all, sum);
+        for (int k = 0; k < 8; ++k) acc[k] = tkv::over_rows(acc[k] * mine, add);
+      }
+      if (share == 0 && row + sub < rows) {
+        const int64_t to = row_out(p, x, ROWS * x.tile + row + sub);
+        *(uintx4*)((T*)p->out + to * TKV_D + c) = pack8<T>(acc * (l == 0.f ? 0.f : 1.f / l));  // (no key: zeros)
+        if (p->lse && c == 0) p->lse[to] = log_sum(m, l);
+      }
       m = kNone;
       l = 0.f;
       acc = (floatx8){0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
@@ -851,10 +855,11 @@ __global__ __launch_bounds__(64 * kWaves, 2) void paged_attn_kernel(PagedParams)
     const Args p = arguments();
     const Parts parts(at, pw, total);
     if (threadIdx.x == 0) __hip_atomic_store(p->arrivals + parts.w0, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-    // (few rows in few parts are one wave's)
-    const bool alone = !together && parts.count <= 4 && at.sq.q_len * walk.group <= 4;
+    const int rows = at.sq.q_len * walk.group - kRows * at.tile;
+    const bool alone = !together && parts.count <= 4 && rows <= 4;  // (one wave's)
     if (alone && i / 2 != wave) continue;
-    join_rows<T, kRows>(p, at, parts, alone ? 0 : wave, alone ? 1 : kWaves);
+    if (rows <= 4 || (rows <= 8 && parts.count > 8)) join_rows<T, kRows, 4>(p, at, parts, alone ? 0 : wave, alone ? 1 : kWaves);
+    else join_rows<T, kRows, 1>(p, at, parts, 4 * wave, 4 * kWaves);
   }
 }
 
