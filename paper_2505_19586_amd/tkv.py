@@ -7,6 +7,7 @@ import ctypes as C
 import itertools
 import operator
 import os
+import struct
 import threading
 
 import numpy as np
@@ -70,6 +71,11 @@ class RopeDesc(C.Structure):
                 ("k_stride_head", C.c_int64), ("v_stride", C.c_int64), ("v_stride_head", C.c_int64)]
 
 
+# A RopeDesc's bytes: packed by `struct` in a fifth of the time that the class takes for its seventeen fields.
+_ROPE_DESC = struct.Struct("Iiiiiiifiiqqqqqq")
+assert _ROPE_DESC.size == C.sizeof(RopeDesc)
+
+
 class PromptDesc(C.Structure):
     _fields_ = [("struct_size", C.c_uint32), ("n_q_heads", C.c_int32), ("n_kv_heads", C.c_int32),
                 ("head_dim", C.c_int32), ("dtype", C.c_int32), ("causal", C.c_int32), ("batch", C.c_int32),
@@ -130,13 +136,13 @@ def lib() -> C.CDLL:
         L.tkv_dense_preference_sizes.argtypes = [C.POINTER(PrefDesc), C.POINTER(sz)]
         L.tkv_dense_preference.argtypes = [C.POINTER(PrefDesc), vp, vp, i32, C.c_float, vp, vp, sz, vp]
         L.tkv_classify_layer.argtypes = [C.POINTER(C.c_float), i32, i32, C.c_float, C.POINTER(C.c_float)]
-        L.tkv_qk_norm_rope.argtypes = [C.POINTER(RopeDesc), i32] + [vp] * 11
-        L.tkv_qk_norm_rope_axes.argtypes = [C.POINTER(RopeDesc), i32] + [vp] * 6 + [i32] + [vp] * 6
+        L.tkv_qk_norm_rope.argtypes = [vp, i32] + [vp] * 11  # (a descriptor's bytes or its reference)
+        L.tkv_qk_norm_rope_axes.argtypes = [vp, i32] + [vp] * 6 + [i32] + [vp] * 6
         L.tkv_paged_cache_sizes.argtypes = [C.POINTER(PagedDesc), C.POINTER(sz)]
-        L.tkv_paged_append.argtypes = [C.POINTER(PagedDesc), C.POINTER(RopeDesc), i32] + [vp] * 6 + [i32] + [vp] * 8
-        L.tkv_paged_gather.argtypes = [C.POINTER(PagedDesc), vp, vp, i32] + [vp] * 4
+        L.tkv_paged_append.argtypes = [vp, vp, i32] + [vp] * 6 + [i32] + [vp] * 8
+        L.tkv_paged_gather.argtypes = [vp, vp, vp, i32] + [vp] * 4
         L.tkv_paged_attn_sizes.argtypes = [C.POINTER(PagedDesc), C.POINTER(sz)]
-        L.tkv_paged_attn.argtypes = [C.POINTER(PagedDesc), vp, vp, i32, i32, i32, vp, vp, vp, vp, i32, vp, vp, i32, C.c_float, vp, sz, vp]
+        L.tkv_paged_attn.argtypes = [vp, vp, vp, i32, i32, i32, vp, vp, vp, vp, i32, vp, vp, i32, C.c_float, vp, sz, vp]
         L.tkv_prompt_attn_sizes.argtypes = [C.POINTER(PromptDesc), C.POINTER(sz)]
         L.tkv_prompt_attn.argtypes = [C.POINTER(PromptDesc)] + [vp] * 9 + [C.c_float, vp, sz, vp]
         L.tkv_quant_attn_decode_shared_sizes.argtypes = [C.POINTER(QuantDesc), C.POINTER(QuantDesc), C.POINTER(sz)]
@@ -187,6 +193,15 @@ def _stream(stream) -> int:
     return stream.cuda_stream if hasattr(stream, "cuda_stream") else int(stream)
 
 
+def _handle(at: int, stream) -> int:
+    """_on_current and _stream in one, for tensors of device number `at`."""
+    if stream is not None:
+        return stream.cuda_stream if hasattr(stream, "cuda_stream") else int(stream)
+    current = torch._C._cuda_getDevice()
+    assert at == current, f"tensors on device {at}, the current device is {current}: make it current or pass a stream of theirs"
+    return torch._C._cuda_getCurrentRawStream(current)
+
+
 def _on_current(t: torch.Tensor, stream) -> None:
     """Without a stream the current device's is used: the tensors have to be that device's."""
     assert stream is not None or t.get_device() == torch._C._cuda_getDevice(), \
@@ -206,6 +221,14 @@ def _like(x: torch.Tensor, dtype, stream) -> torch.Tensor:
     if stream is not None:
         return _new(x.shape, dtype, x.device, stream)
     return torch.empty_like(x, dtype=dtype, memory_format=torch.contiguous_format)
+
+
+def _given(out: torch.Tensor | None, x: torch.Tensor, dtype, at: int, stream) -> torch.Tensor:
+    """An output of x's shape, where the caller gave none a new one."""
+    if out is None:
+        return _like(x, dtype, stream)
+    assert out.dtype == dtype and out.shape == x.shape and out.is_contiguous() and out.get_device() == at
+    return out
 
 
 class _Workspaces:
@@ -667,7 +690,7 @@ def rope_axes(sections, interleaved: bool = False) -> bytes:
 
 def _rotation(q, k, positions, inv_freq, axis_of, norm, q_weight, k_weight, eps, interleaved, v, out_dtype, n_q_heads=None):
     """What qk_norm_rope and PagedCache.append check and describe alike (q None: its heads count as n_q_heads):
-    the descriptor and n_axes."""
+    the descriptor's bytes, its rotary_dim and n_axes."""
     shape_k = k.shape
     t, hkv, ch = shape_k
     dt, at = k.dtype, k.get_device()  # (numbers of devices compare in a third of the time of devices)
@@ -696,8 +719,8 @@ def _rotation(q, k, positions, inv_freq, axis_of, norm, q_weight, k_weight, eps,
         assert w is None or (w.shape == (ch,) and w.is_contiguous() and w.dtype == dt and w.get_device() == at)
     # (an axis of one element: torch leaves its stride to chance)
     by_t, by_q, by_k = t > 1, n_q_heads > 1, hkv > 1
-    return RopeDesc(C.sizeof(RopeDesc), n_q_heads, hkv, ch, _DTYPES.get(dt, -1), _DTYPES.get(out_dtype, -1), norm, eps, rot, interleaved,
-                    by_t * sq[0], by_q * sq[1], by_t * sk[0], by_k * sk[1], by_t * sv[0], by_k * sv[1]), n_axes
+    return _ROPE_DESC.pack(_ROPE_DESC.size, n_q_heads, hkv, ch, _DTYPES.get(dt, -1), _DTYPES.get(out_dtype, -1), norm, eps, rot, interleaved,
+                           by_t * sq[0], by_q * sq[1], by_t * sk[0], by_k * sk[1], by_t * sv[0], by_k * sv[1]), rot, n_axes
 
 
 def qk_norm_rope(q: torch.Tensor, k: torch.Tensor, positions: torch.Tensor | None, inv_freq: torch.Tensor | None, *,
@@ -709,29 +732,26 @@ def qk_norm_rope(q: torch.Tensor, k: torch.Tensor, positions: torch.Tensor | Non
     allowed), positions int32 [T], inv_freq float32 [R/2] (None: no rotation) -> contiguous (q_out, k_out, v_out or
     None) in out_dtype (default: the inputs').  With axis_of (bytes or small numbers, an axis for every frequency; see rope_axes) positions
     are int32 [axes, T]: tkv_qk_norm_rope_axes."""
-    shape_q, shape_k = q.shape, k.shape
-    dt, at = q.dtype, q.get_device()
-    _on_current(q, stream)
+    shape_q, at = q.shape, q.get_device()
+    handle = _handle(at, stream)
     if axis_of is not None:
         axis_of = bytes(axis_of)
     if out_dtype is None:
-        out_dtype = next((x.dtype for x in (q_out, k_out, v_out) if x is not None), dt)
-    desc, n_axes = _rotation(q, k, positions, inv_freq, axis_of, norm, q_weight, k_weight, eps, interleaved, v, out_dtype)
-    for o, shape in ((q_out, shape_q), (k_out, shape_k), (v_out, shape_k if v is not None else None)):
-        assert o is None or (o.dtype == out_dtype and o.shape == shape and o.is_contiguous() and o.get_device() == at)
-    if q_out is None:
-        q_out = _like(q, out_dtype, stream)
-    if k_out is None:
-        k_out = _like(k, out_dtype, stream)
-    if v_out is None and v is not None:
-        v_out = _like(v, out_dtype, stream)
-    pos, freq = (_ptr(positions), _ptr(inv_freq)) if desc.rotary_dim else (0, 0)
-    outs = q_out.data_ptr(), k_out.data_ptr(), _ptr(v_out), _stream(stream)
+        out_dtype = next((x.dtype for x in (q_out, k_out, v_out) if x is not None), q.dtype)
+    desc, rot, n_axes = _rotation(q, k, positions, inv_freq, axis_of, norm, q_weight, k_weight, eps, interleaved, v, out_dtype)
+    q_out = _given(q_out, q, out_dtype, at, stream)
+    k_out = _given(k_out, k, out_dtype, at, stream)
+    if v is not None:
+        v_out = _given(v_out, v, out_dtype, at, stream)
+    else:
+        assert v_out is None
+    pos, freq = (positions.data_ptr(), inv_freq.data_ptr()) if rot else (0, 0)
+    outs = q_out.data_ptr(), k_out.data_ptr(), _ptr(v_out), handle
     if axis_of is None:
-        _check(lib().tkv_qk_norm_rope(C.byref(desc), shape_q[0], q.data_ptr(), k.data_ptr(), _ptr(v), pos, freq, _ptr(q_weight),
+        _check(lib().tkv_qk_norm_rope(desc, shape_q[0], q.data_ptr(), k.data_ptr(), _ptr(v), pos, freq, _ptr(q_weight),
                                       _ptr(k_weight), *outs), "tkv_qk_norm_rope")
     else:
-        _check(lib().tkv_qk_norm_rope_axes(C.byref(desc), shape_q[0], q.data_ptr(), k.data_ptr(), _ptr(v), pos, freq, axis_of, n_axes,
+        _check(lib().tkv_qk_norm_rope_axes(desc, shape_q[0], q.data_ptr(), k.data_ptr(), _ptr(v), pos, freq, axis_of, n_axes,
                                            _ptr(q_weight), _ptr(k_weight), *outs), "tkv_qk_norm_rope_axes")
     return q_out, k_out, v_out
 
@@ -772,6 +792,7 @@ class PagedCache:
         self.k_pages, self.v_pages, self.dtype = k_pages, v_pages, dtype
         self.device, self._at = k_pages.device, k_pages.get_device()
         self._pages = k_pages.data_ptr(), v_pages.data_ptr()
+        self._desc_at = C.addressof(self.desc)
         self._rows = (n_q_heads, head_dim), (n_kv_heads, head_dim)
         self._workspaces = _Workspaces(self.workspace_bytes, torch.device("cuda", self._at), at_once=False, zeros=12288)  # (a cache that is only filled needs none)
 
@@ -787,29 +808,30 @@ class PagedCache:
         too."""
         t, at = k.shape[0], self._at
         assert k.get_device() == at and v is not None and k.shape[1:] == self._rows[1] and (q is None or q.shape[1:] == self._rows[0])
-        _on_current(k, stream)
+        handle = _handle(at, stream)
         self._slots(slots, t)
         if axis_of is not None:
             axis_of = bytes(axis_of)
-        desc, n_axes = _rotation(q, k, positions, inv_freq, axis_of, norm, q_weight, k_weight, eps, interleaved, v, self.dtype,
-                                 self.desc.n_q_heads)
-        if q is None:
+        dt = self.dtype
+        desc, rot, n_axes = _rotation(q, k, positions, inv_freq, axis_of, norm, q_weight, k_weight, eps, interleaved, v, dt,
+                                      self._rows[0][0])
+        if q is not None:
+            q_out = _given(q_out, q, dt, at, stream)
+        else:
             assert q_out is None
-        elif q_out is None:
-            q_out = _like(q, self.dtype, stream)
-        for o, x in ((q_out, q), (k_out, k)):
-            assert o is None or (o.dtype == self.dtype and o.shape == x.shape and o.is_contiguous() and o.get_device() == at)
-        pos, freq = (_ptr(positions), _ptr(inv_freq)) if desc.rotary_dim else (0, 0)
-        _check(lib().tkv_paged_append(C.byref(self.desc), C.byref(desc), t, _ptr(q), k.data_ptr(), v.data_ptr(), pos, freq, axis_of,
+        if k_out is not None:
+            _given(k_out, k, dt, at, stream)
+        pos, freq = (positions.data_ptr(), inv_freq.data_ptr()) if rot else (0, 0)
+        _check(lib().tkv_paged_append(self._desc_at, desc, t, _ptr(q), k.data_ptr(), v.data_ptr(), pos, freq, axis_of,
                                       n_axes, _ptr(q_weight), _ptr(k_weight), slots.data_ptr(), _ptr(q_out), _ptr(k_out),
-                                      *self._pages, _stream(stream)), "tkv_paged_append")
+                                      *self._pages, handle), "tkv_paged_append")
         return q_out
 
     def gather(self, slots: torch.Tensor, k_out: torch.Tensor | None = None, v_out: torch.Tensor | None = None, stream=None):
         """tkv_paged_gather: the tokens at slots (int32 [T], below 0: zeros) as contiguous k, v [T, Hkv, 128]."""
         t = slots.shape[0]
         self._slots(slots, t)
-        _on_current(slots, stream)
+        handle = _handle(self._at, stream)
         outs = []
         for o in (k_out, v_out):
             if o is None:
@@ -817,8 +839,8 @@ class PagedCache:
             else:
                 assert o.dtype == self.dtype and o.shape == (t, *self._rows[1]) and o.is_contiguous() and o.get_device() == self._at
             outs.append(o)
-        _check(lib().tkv_paged_gather(C.byref(self.desc), *self._pages, t, slots.data_ptr(), outs[0].data_ptr(), outs[1].data_ptr(),
-                                      _stream(stream)), "tkv_paged_gather")
+        _check(lib().tkv_paged_gather(self._desc_at, *self._pages, t, slots.data_ptr(), outs[0].data_ptr(), outs[1].data_ptr(),
+                                      handle), "tkv_paged_gather")
         return outs[0], outs[1]
 
     def attend(self, q: torch.Tensor, sm_scale: float, page_table: torch.Tensor, k_lens: torch.Tensor, *,
@@ -828,10 +850,10 @@ class PagedCache:
         own among them; q_starts int32 [B + 1]: where each sequence's rows of q begin, max_q_len of them at most (both None: row b is
         sequence b's only one).  Returns out [T, Hq, 128], or (out, lse [T, Hq]) where lse is True or a float32 tensor.  Rows of no
         sequence are left as they were (a new out has zeros there)."""
-        t, at, d = q.shape[0], self._at, self.desc
+        t, at = q.shape[0], self._at
         b, each = page_table.shape
         assert q.dtype == self.dtype and q.shape[1:] == self._rows[0] and q.is_contiguous() and q.get_device() == at
-        _on_current(q, stream)
+        handle = _handle(at, stream)
         assert page_table.dtype == torch.int32 and page_table.is_contiguous() and page_table.get_device() == at
         assert k_lens.dtype == torch.int32 and k_lens.shape == (b,) and k_lens.is_contiguous() and k_lens.get_device() == at
         if q_starts is None:
@@ -848,15 +870,14 @@ class PagedCache:
         else:
             assert out.dtype == q.dtype and out.shape == q.shape and out.is_contiguous() and out.get_device() == at
         if new_lse:
-            lse = _new((t, d.n_q_heads), torch.float32, q.device, stream, -float("inf") if fill else None)
+            lse = _new(q.shape[:2], torch.float32, q.device, stream, -float("inf") if fill else None)
         elif lse is False or lse is None:
             lse = None
         else:
             assert lse.dtype == torch.float32 and lse.shape == q.shape[:2] and lse.is_contiguous() and lse.get_device() == at
-        handle = _stream(stream)
         with self._workspaces.lock:
             workspace = self._workspaces.of(handle, stream)
-            status = lib().tkv_paged_attn(C.byref(d), *self._pages, b, t, int(max_q_len), q.data_ptr(), out.data_ptr(), _ptr(lse),
+            status = lib().tkv_paged_attn(self._desc_at, *self._pages, b, t, int(max_q_len), q.data_ptr(), out.data_ptr(), _ptr(lse),
                                           page_table.data_ptr(), each, k_lens.data_ptr(), _ptr(q_starts), clear, float(sm_scale),
                                           workspace.data_ptr(), self.workspace_bytes, handle)
         _check(status, "tkv_paged_attn")
