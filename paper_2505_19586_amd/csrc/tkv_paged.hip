@@ -92,6 +92,7 @@ struct PagedParams {
   float* ml;                // [2 per wave][rows of a tile][2] (reference, sum)
   uint32_t* arrivals;       // [wave] parts, of the item whose first cut lies behind its range, that have come in
   int32_t n_tokens, batch, max_q_len, hq, group, pages_each;
+  uint32_t per_group;  // 2^32 / group, rounded up: rows / group without a division
   int32_t workgroups;
   int32_t clear_rest;  // rows of no sequence get zeros
   float scale2;        // sm_scale * log2(e)
@@ -120,6 +121,19 @@ struct Place {
   uint32_t start;     // of the item's tiles, among all
   int32_t h, tile, t; // KV head, tile of rows, tile of keys
 };
+
+// Every lane: f over the lanes up to it (0 where there is none).  By data-parallel primitives: rows of sixteen, then their last lanes'
+// values into the rows behind.
+template <typename F>
+__device__ inline uint32_t scan(uint32_t x, F f) {
+  x = f(x, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x111, 0xF, 0xF, true));  // row_shr: 1, 2, 4, 8
+  x = f(x, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x112, 0xF, 0xF, true));
+  x = f(x, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x114, 0xF, 0xF, true));
+  x = f(x, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x118, 0xF, 0xF, true));
+  x = f(x, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x142, 0xA, 0xF, false));  // row_bcast: 15 into rows 1 and 3, 31 into 2 and 3
+  x = f(x, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x143, 0xC, 0xF, false));
+  return x;
+}
 
 template <int TK, int ROWS>
 struct Walk {
@@ -151,17 +165,11 @@ struct Walk {
       }
     }
     count = (uint32_t)(key_tiles(k_len) * row_tiles(q_len)) * (uint32_t)p->pages.hkv;  // (no rows: 0)
-    uint32_t sum = count;
-    int32_t most = count ? key_tiles(k_len) : 1;
-#pragma unroll
-    for (int d = 1; d < 64; d *= 2) {
-      const uint32_t x = __shfl_up(sum, d, 64);
-      if (lane >= d) sum += x;
-      most = max(most, __shfl_xor(most, d, 64));
-    }
+    const uint32_t sum = scan(count, [](uint32_t a, uint32_t b) { return a + b; });
     first = before + sum - count;
     all = before + (uint32_t)__builtin_amdgcn_readlane((int)sum, 63);
-    longest = max(longest, __builtin_amdgcn_readfirstlane(most));
+    const uint32_t most = scan(count ? (uint32_t)key_tiles(k_len) : 0u, [](uint32_t a, uint32_t b) { return max(a, b); });
+    longest = max(longest, __builtin_amdgcn_readlane((int)most, 63));
   }
   __device__ uint32_t total() {
     while (chunk + 64 < batch) load(chunk + 64, all);
@@ -215,14 +223,23 @@ struct Plan {
     stop = min(min(from + ((uint32_t)(64 / PER) << log_step), end), walk.all);
     const int lane = threadIdx.x % 64;
     const uint32_t g = min(from + ((uint32_t)(lane / PER) << log_step), stop - 1u);
-    int l = 0;  // the last sequence that begins at or before it (one without tiles shares its successor's beginning)
+    // its sequence: nearly always the first one's, otherwise the last that begins at or before it (one without tiles shares its
+    // successor's beginning)
+    const uint64_t here = __builtin_amdgcn_ballot_w64(walk.first <= from && from < walk.first + walk.count);
+    int l = here ? __builtin_ctzll(here) : 0;
+    int32_t k_len = __builtin_amdgcn_readlane(walk.k_len, l), q_len = __builtin_amdgcn_readlane(walk.q_len, l);
+    uint32_t first = (uint32_t)__builtin_amdgcn_readlane((int)walk.first, l);
+    if (stop > first + (uint32_t)__builtin_amdgcn_readlane((int)walk.count, l)) {
+      l = 0;
 #pragma unroll
-    for (int d = 32; d > 0; d /= 2) {
-      const uint32_t f = (uint32_t)__shfl((int)walk.first, l + d, 64);
-      if (f <= g) l += d;
+      for (int d = 32; d > 0; d /= 2) {
+        const uint32_t f = (uint32_t)__shfl((int)walk.first, l + d, 64);
+        if (f <= g) l += d;
+      }
+      k_len = __shfl(walk.k_len, l, 64);
+      q_len = __shfl(walk.q_len, l, 64);
+      first = (uint32_t)__shfl((int)walk.first, l, 64);
     }
-    const int32_t k_len = __shfl(walk.k_len, l, 64), q_len = __shfl(walk.q_len, l, 64);
-    const uint32_t first = (uint32_t)__shfl((int)walk.first, l, 64);
     const uint32_t key_tiles = (uint32_t)walk.key_tiles(k_len), row_tiles = (uint32_t)max(1, walk.row_tiles(q_len));
     const uint32_t in = g - first, item = in / key_tiles, h = min(item / row_tiles, (uint32_t)p->pages.hkv - 1u);
     const int32_t key = 16 * ((int32_t)(in - item * key_tiles) * PER + lane % PER);
@@ -599,9 +616,14 @@ struct PartStore {
   }
 };
 
+// The token of a row.  (Exact below 2^32 / group rows; 2^32 / 1 does not fit, and is given as 0.)
+__device__ inline int32_t row_token(Args p, int32_t row) {
+  const uint32_t m = p->per_group;
+  return m == 0u ? row : (int32_t)__umulhi((uint32_t)row, m);
+}
 // Where a finished row of an item goes, and the logarithm of its sum.
 __device__ inline int64_t row_out(Args p, const Place& x, int row) {
-  const int group = p->group, token = row / group, head = row - token * group;
+  const int group = p->group, token = row_token(p, row), head = row - token * group;
   return (int64_t)(x.sq.q_start + token) * p->hq + x.h * group + head;
 }
 __device__ inline float log_sum(float ref, float sum) {
@@ -711,11 +733,12 @@ __global__ __launch_bounds__(64 * kWaves, 2) void paged_attn_kernel(PagedParams)
   auto reset = [&](const Place& at) {
     const int rows = at.sq.q_len * walk.group, ahead = at.sq.k_len - at.sq.q_len;
     r.scale2 = arguments()->scale2;
-    r.limit_low = at.tile * kRows / walk.group + ahead;
+    const Args p = arguments();
+    r.limit_low = row_token(p, at.tile * kRows) + ahead;
 #pragma unroll
     for (int m = 0; m < NT; ++m) {
       const int row = min(at.tile * kRows + 16 * m + col, rows - 1);
-      r.limit[m] = row / walk.group + ahead;
+      r.limit[m] = row_token(p, row) + ahead;
       r.ref[m] = kNone;
       r.sum[m] = 0.f;
 #pragma unroll
@@ -1025,7 +1048,8 @@ extern "C" int32_t tkv_paged_attn(const tkv_paged_desc* d, const void* k_pages, 
   p.clear_rest = q_starts && clear_rest;
   // Numbers of tiles are 32 bits, whatever the device's arrays hold: tiles of 16 rows and 32 keys, the smallest.
   max_q_len = std::min(max_q_len, n_tokens);
-  if ((int64_t)max_q_len * p.group > (1 << 24)) return TKV_E_UNSUPPORTED;
+  if ((int64_t)max_q_len * p.group > (1 << 24) || (int64_t)max_q_len * p.group * p.group >= ((int64_t)1 << 32)) return TKV_E_UNSUPPORTED;
+  p.per_group = p.group == 1 ? 0u : (uint32_t)((((uint64_t)1 << 32) + p.group - 1) / p.group);
   const int64_t row_tiles = (int64_t)batch * (((int64_t)max_q_len * p.group + 15) / 16), key_tiles = (((int64_t)pages_each * d->page_size) >> 5) + 1;
   if (row_tiles * d->n_kv_heads >= ((int64_t)1 << 31) || row_tiles * d->n_kv_heads * key_tiles >= ((int64_t)1 << 31)) return TKV_E_UNSUPPORTED;
   const int64_t rows = (int64_t)max_q_len * p.group;
