@@ -25,7 +25,8 @@
  *   - Calls enqueue work on the given hipStream_t (passed as void*) and return
  *     without synchronizing.  Sequence lengths live in caller-owned HOST int32
  *     arrays; kernels receive them by value, so the arrays may be changed as soon as
- *     a call returns.  At most TKV_MAX_BATCH sequences per call.
+ *     a call returns.  At most TKV_MAX_BATCH sequences per call.  (Paged caches: on the
+ *     device, any number of sequences.)
  *   - fp16 is IEEE binary16 everywhere.  head_dim must be 128, the quantization
  *     group g 32 or 64.  n_q_heads / n_kv_heads: any number from 1 to 8 (quantized layers:
  *     groups of 5 to 8 are one workgroup per chunk, or two of up to 4 heads that each read the
@@ -570,7 +571,7 @@ typedef struct {
  * 4 bits: k_pages, v_pages are uint8 [n_pages][Hkv][68 * page_size]: the codes of all of a head's tokens, 64 bytes each (channel 2i in
  * the low half of byte i), then the scales of all of them, 4 bytes each: byte u is the exponent + 127 of channels 32u to
  * 32u + 31.  A code is a 4-bit floating-point number, sign, two bits of exponent, one of mantissa (0, 0.5, 1, 1.5, 2, 3, 4, 6), and stands
- * for itself times 2^exponent; a scale of 255 stands for NaN.
+ * for itself times 2^exponent; a scale of 255 stands for NaN, 0 is not used.
  */
 
 /* Bytes of k_pages, and of v_pages, without room between rows. */
@@ -613,14 +614,18 @@ int32_t tkv_paged_attn_sizes(const tkv_paged_desc* desc, size_t* workspace_bytes
  * out = softmax(sm_scale q.k) v; a token that sees no key yields zeros, and -inf in lse.
  * q, out [n_tokens][Hq][128] contiguous; lse float32 [n_tokens][Hq] (natural logarithm of the sum of exponentials) or NULL.  Rows of out and
  * lse that belong to no sequence (in front of the first, behind the last) are left as they were, or with clear_rest = 1 get zeros and
- * -inf.  max_q_len: the most queries that a sequence has, as the host knows it; q_starts that say more
- * count as that many.  batch * (tiles of 16 rows of max_q_len * Hq / Hkv) * Hkv * (pages_each * page_size / 32 + 1) < 2^31.
- * Keys behind a sequence's last are never used, whatever their slots hold.  A page number outside the cache stands for rows of zeros; k_lens
- * beyond pages_each * page_size, or below 0, count as that, or as 0.
+ * -inf.  max_q_len: the most queries that a sequence has, as the host knows it; where q_starts say more, that many count.
+ * Limits (TKV_E_UNSUPPORTED beyond): pages_each * page_size <= 2^30, max_q_len * (Hq/Hkv)^2 < 2^32, and batch * Hkv *
+ * ceil(max_q_len * (Hq/Hkv) / 16) * (pages_each * page_size / 32 + 1) < 2^31.
+ * Keys behind a sequence's last are never used, whatever their slots hold; a non-finite value of a later token of the same call may still
+ * reach the tokens before it.  A page number outside the cache stands for rows of zeros; k_lens beyond pages_each * page_size, or below 0,
+ * count as that, or as 0.
  * Products in desc->dtype with float32 sums (4 bits: of what the codes stand for, exactly); softmax statistics in float32.
  * 0 < sm_scale <= 2.3e38; logits (sm_scale q.k) of magnitude up to 2^26 are safe.  The result is the same bit for bit from call to call
- * (on streams that may use as many compute units).  Addresses of pages, q, out and workspace are multiples of 16 bytes; concurrent calls
- * need separate workspaces.
+ * (on streams that may use as many compute units).  Addresses of pages, q, out and workspace are multiples of 16 bytes; out and lse
+ * must not overlap the inputs; concurrent calls need separate workspaces.
+ * Up to about 64 tokens of a sequence this is the shorter way (64 tokens of 32/8 heads over 2000 in 16 bits 31 us, over 65536 in 4 bits 138);
+ * for more, tkv_paged_gather and tkv_prompt_attn (333 over 65536 in 16 bits 498 us, against 1035).
  */
 int32_t tkv_paged_attn(const tkv_paged_desc* desc, const void* k_pages, const void* v_pages, int32_t batch, int32_t n_tokens,
                        int32_t max_q_len, const void* q, void* out, float* lse, const int32_t* page_table, int32_t pages_each,

@@ -250,7 +250,9 @@ class _Workspaces:
         w = None if captured else self._of.get(handle)
         if w is None:
             w = _new(self._bytes, torch.uint8, self._device, stream)
-            if self._zeros:
+            if self._zeros and stream is None:
+                w[-self._zeros:].zero_()
+            elif self._zeros:
                 with torch.cuda.stream(stream if hasattr(stream, "cuda_stream") else torch.cuda.ExternalStream(handle, device=self._device)):
                     w[-self._zeros:].zero_()
             if not captured:

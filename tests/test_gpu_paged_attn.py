@@ -381,3 +381,136 @@ def test_prompt_then_chunk_then_decode():
             kk, vv = cache.gather(slots[:j])
             _compare(out, lse, _f64(x), _f64(kk), _f64(vv), torch.float16)
             assert (lse - want_lse).abs().max() <= 2e-5
+
+
+@BOTH
+def test_one_kv_head_and_a_long_sequence(bits):
+    """More workgroups than an item's parts may be; rows of all kinds of joins."""
+    for hq, n in ((4, 20011), (12, 30000), (32, 9999), (64, 5000)):
+        print(f"case {hq}/1 heads over {n} {bits} bits", flush=True)
+        _run([1], [n], hq, 1, 64, bits, seed=hq, starts=False)
+
+
+@BOTH
+def test_items_of_every_size_beside_each_other(bits):
+    """Cuts at every place of an item: in its first tile, its last, at its beginning; workgroups in one item and in many."""
+    rng = np.random.default_rng(3)
+    for case in range(6):
+        b = int(rng.integers(2, 90))
+        lens = [int(n) for n in np.where(rng.random(b) < 0.2, rng.integers(500, 4000, b), rng.integers(0, 200, b))]
+        q_lens = [int(n) for n in rng.integers(0, 4, b)]
+        hq, hkv = [(8, 2), (8, 8), (16, 1), (6, 3)][case % 4]
+        print(f"case mixed {case} {b} sequences {bits} bits", flush=True)
+        _run(q_lens, lens, hq, hkv, 16, bits, seed=case)
+
+
+@BOTH
+def test_pools_beyond_4_gib(bits):
+    """Pages at the far end of a pool of more than 2^32 bytes, and of more than 2^31 elements."""
+    hkv, page = 8, 64
+    n_pages = 40000 if bits == 16 else 135000          # 5.2 GB, 4.7 GB each of keys and values
+    shape, dt = ((n_pages, hkv, page, 128), torch.float16) if bits == 16 else ((n_pages, hkv, 68 * page), torch.uint8)
+    pages = [torch.empty(shape, dtype=dt, device="cuda") for _ in range(2)]
+    cache = tkv.PagedCache(n_q_heads=16, n_kv_heads=hkv, page_size=page, bits=bits, k_pages=pages[0], v_pages=pages[1])
+    n = 200
+    table = torch.tensor([[n_pages - 1, 3, n_pages - 2, n_pages // 2 + 7]], dtype=torch.int32)
+    slots = torch.from_numpy(paged.sequence_slots(table[0].numpy(), n, page).astype(np.int32)).cuda()
+    k, v = (torch.randn(n, hkv, 128, device="cuda").half() for _ in range(2))
+    cache.append(None, k, v, slots)
+    got = cache.gather(slots)
+    if bits == 16:
+        assert torch.equal(got[0], k) and torch.equal(got[1], v)
+    q = torch.randn(1, 16, 128, device="cuda").half()
+    out, lse = cache.attend(q, SM, table.cuda(), torch.tensor([n], device="cuda", dtype=torch.int32), lse=True)
+    torch.cuda.synchronize()
+    _compare(out, lse, _f64(q), _f64(got[0]), _f64(got[1]), torch.float16)
+
+
+def test_stream_with_compute_unit_mask():
+    """On part of the machine there are fewer ranges."""
+    import ctypes as C
+    print("case masked stream", flush=True)
+    hip = C.CDLL("libamdhip64.so")
+    create = hip.hipExtStreamCreateWithCUMask
+    create.argtypes = [C.POINTER(C.c_void_p), C.c_uint32, C.POINTER(C.c_uint32)]
+    create.restype = C.c_int
+    mask = (C.c_uint32 * 8)(0xFFFF0000, 0xFFFFFFFF, 0xFFFFFFFF, 0x0000FFFF, 0, 0, 0, 0)   # 96 units
+    handle = C.c_void_p()
+    if create(C.byref(handle), 8, mask) != 0 or not handle.value:
+        pytest.skip("streams with a compute-unit mask are not available")
+    try:
+        for bits in (16, 4):
+            pages, table, rows = _filled([3000, 700], 2, 32, bits, torch.float16, seed=13)
+            cache = tkv.PagedCache(n_q_heads=8, n_kv_heads=2, page_size=32, bits=bits, k_pages=pages[0], v_pages=pages[1])
+            q = torch.randn(2, 8, 128, device="cuda").half()
+            lens = torch.tensor([3000, 700], device="cuda", dtype=torch.int32)
+            torch.cuda.synchronize()
+            out, lse = cache.attend(q, SM, table, lens, lse=True, stream=handle.value)
+            again = cache.attend(q, SM, table, lens, stream=handle.value)
+            torch.cuda.synchronize()
+            assert torch.equal(out, again)
+            for b, (k, v) in enumerate(rows):
+                _compare(out[b:b + 1], lse[b:b + 1], _f64(q[b:b + 1]), k, v, torch.float16)
+    finally:
+        torch.cuda.synchronize()
+        hip.hipStreamDestroy(handle)
+
+
+def test_threads_with_streams_of_their_own_and_one_object():
+    import threading
+    lens = [[900, 33], [5, 2100]]
+    made = [_filled(n, 2, 32, 16, torch.float16, seed=20 + i) for i, n in enumerate(lens)]
+    pages = [torch.cat((made[0][0][i], made[1][0][i])) for i in range(2)]
+    cache = tkv.PagedCache(n_q_heads=8, n_kv_heads=2, page_size=32, k_pages=pages[0], v_pages=pages[1])
+    tables = [made[0][1], torch.where(made[1][1] < 10**6, made[1][1] + made[0][0][0].shape[0], made[1][1])]
+    q = [torch.randn(2, 8, 128, device="cuda").half() for _ in range(2)]
+    k_lens = [torch.tensor(n, device="cuda", dtype=torch.int32) for n in lens]
+    want = [cache.attend(q[i], SM, tables[i], k_lens[i]) for i in range(2)]
+    torch.cuda.synchronize()
+    bad = []
+
+    def work(i):
+        torch.cuda.set_device(0)
+        with torch.cuda.stream(torch.cuda.Stream()):
+            for _ in range(50):
+                if not torch.equal(cache.attend(q[i], SM, tables[i], k_lens[i]), want[i]):
+                    bad.append(i)
+            torch.cuda.current_stream().synchronize()
+
+    threads = [threading.Thread(target=work, args=(i,)) for i in range(2)]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    assert not bad
+    for i in range(2):
+        for b, (k, v) in enumerate(made[i][2]):
+            ref, _ = prompt_attention(_f64(q[i][b:b + 1]), k, v, SM)
+            assert np.abs(_f64(want[i][b:b + 1]) - ref).max() < 2e-3
+
+
+def test_two_graphs_and_eager_calls_of_one_object():
+    """Graphs captured from one object replay beside each other on streams of their own."""
+    pages, table, rows = _filled([3000, 700], 2, 32, 16, torch.float16, seed=14)
+    cache = tkv.PagedCache(n_q_heads=8, n_kv_heads=2, page_size=32, k_pages=pages[0], v_pages=pages[1])
+    lens = torch.tensor([3000, 700], device="cuda", dtype=torch.int32)
+    qs = [torch.randn(2, 8, 128, device="cuda").half() for _ in range(3)]
+    want = [cache.attend(q, SM, table, lens, lse=True) for q in qs]
+    graphs, outs = [], []
+    for q in qs[:2]:
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g):
+            outs.append(cache.attend(q, SM, table, lens, lse=True))
+        graphs.append(g)
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    for _ in range(10):
+        for o in outs:
+            o[0].zero_()
+        torch.cuda.synchronize()
+        for g, s in zip(graphs, streams):
+            with torch.cuda.stream(s):
+                g.replay()
+        eager = cache.attend(qs[2], SM, table, lens, lse=True)
+        torch.cuda.synchronize()
+        for got, w in zip((*outs, eager), want):
+            assert torch.equal(got[0], w[0]) and torch.equal(got[1], w[1])

@@ -122,7 +122,10 @@ def _attn(L, desc=None, ptr=None, batch=3, n=3, most=1, each=7, scale=0.1, ws=1 
 
 @pytest.mark.parametrize("kw,status", [
     (dict(batch=-1), -1), (dict(n=-1), -1), (dict(n=4), -1), (dict(most=0), -1), (dict(most=2), -1), (dict(each=-1), -1),
-    (dict(each=1 << 26), -2), (dict(scale=0.0), -1), (dict(scale=-1.0), -1), (dict(scale=float("nan")), -1), (dict(scale=INF), -1),
+    (dict(each=1 << 26), -2), (dict(each=(1 << 24) + 1), -2),
+    (dict(each=1 << 24, ws=8), -4), (dict(batch=8, n=8, each=1 << 24), -2), (dict(batch=4000, n=4000, each=2048, ws=8), -4),
+    (dict(n=1 << 23, most=1 << 23, ptr=dict(q_starts=A)), -2), (dict(desc=dict(n_q_heads=1024, n_kv_heads=1), n=4096, most=4096, ptr=dict(q_starts=A)), -2),
+    (dict(desc=dict(n_q_heads=1024, n_kv_heads=1), n=4095, most=9999, ws=8, ptr=dict(q_starts=A)), -4), (dict(scale=0.0), -1), (dict(scale=-1.0), -1), (dict(scale=float("nan")), -1), (dict(scale=INF), -1),
     (dict(scale=3e38), -1), (dict(ws=8), -4), (dict(ptr=dict(workspace=0)), -1), (dict(ptr=dict(workspace=A + 4)), -1),
     (dict(ptr=dict(q=0)), -1), (dict(ptr=dict(q=A + 8)), -1), (dict(ptr=dict(out=0)), -1), (dict(ptr=dict(out=A + 2)), -1),
     (dict(ptr=dict(lse=A + 2)), -1), (dict(ptr=dict(table=0)), -1), (dict(ptr=dict(table=A + 1)), -1), (dict(ptr=dict(k_lens=0)), -1),
