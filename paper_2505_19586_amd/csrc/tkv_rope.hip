@@ -198,14 +198,17 @@ __global__ __launch_bounds__(256) void qk_norm_rope_kernel(RopeParams p) {
           u = __builtin_fmaf(u0, c, -(w0 * s));
           w = __builtin_fmaf(u0, s, w0 * c);
         };
+        if (p.interleaved) {
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-          if (p.interleaved) {
-            float u = i < 4 ? x[2 * i] : y[2 * i - 8], w = i < 4 ? x[2 * i + 1] : y[2 * i - 7];
-            turn(u, w, cs[i], sn[i]);
-            if (i < 4) x[2 * i] = u, x[2 * i + 1] = w;
-            else y[2 * i - 8] = u, y[2 * i - 7] = w;
-          } else {
+          for (int i = 0; i < 4; ++i) {
+            float x0 = x[2 * i], x1 = x[2 * i + 1], y0 = y[2 * i], y1 = y[2 * i + 1];
+            turn(x0, x1, cs[i], sn[i]);
+            turn(y0, y1, cs[4 + i], sn[4 + i]);
+            x[2 * i] = x0, x[2 * i + 1] = x1, y[2 * i] = y0, y[2 * i + 1] = y1;
+          }
+        } else {
+#pragma unroll
+          for (int i = 0; i < 8; ++i) {
             float u = x[i], w = y[i];
             turn(u, w, cs[i], sn[i]);
             x[i] = u, y[i] = w;
