@@ -939,13 +939,14 @@ int32_t launch_rows(PagedParams& p, int64_t rows, int units, hipStream_t s) {
   return launch_attn<T, BITS, 2>(p, units, s);
 }
 
-// Whether rows of 128 elements at p s[0] + h s[1] + t s[2] do not overlap, each axis beyond all that smaller strides span.
+// Whether rows of 128 elements at p s[0] + h s[1] + t s[2] do not overlap, each axis beyond all that smaller strides span, and end below
+// 2^62.
 bool rows_apart(const int64_t* s, const int64_t (&count)[3]) {
   int order[3] = {0, 1, 2};
   std::sort(order, order + 3, [&](int a, int b) { return s[a] < s[b]; });
   int64_t span = TKV_D;
   for (int i : order) {
-    if (count[i] > 1 && s[i] < span) return false;
+    if (count[i] > 1 && (s[i] < span || s[i] > ((int64_t)1 << 60) / count[i])) return false;
     if (count[i] > 1) span += s[i] * (count[i] - 1);
   }
   return true;

@@ -195,6 +195,7 @@ def _stream(stream) -> int:
 
 def _handle(at: int, stream) -> int:
     """_on_current and _stream in one, for tensors of device number `at`."""
+    assert at >= 0, "tensors of a GPU"
     if stream is not None:
         return stream.cuda_stream if hasattr(stream, "cuda_stream") else int(stream)
     current = torch._C._cuda_getDevice()
@@ -679,6 +680,7 @@ def rope_axes(sections, interleaved: bool = False) -> bytes:
     """The axis of each frequency, for `axis_of`: sections[a] of them belong to axis a, one section after the other, or
     (interleaved) the axes in turn while they have any left."""
     left = [int(n) for n in sections]
+    assert all(n >= 0 for n in left)
     if not interleaved:
         return bytes(a for a, n in enumerate(left) for _ in range(n))
     out = []
@@ -849,8 +851,8 @@ class PagedCache:
                q_starts: torch.Tensor | None = None, max_q_len: int | None = None, out: torch.Tensor | None = None,
                lse: bool | torch.Tensor = False, stream=None):
         """tkv_paged_attn: q [T, Hq, 128]; page_table int32 [B, pages], k_lens int32 [B]: each sequence's pages and tokens, the queries'
-        own among them; q_starts int32 [B + 1]: where each sequence's rows of q begin, max_q_len of them at most (both None: row b is
-        sequence b's only one).  Returns out [T, Hq, 128], or (out, lse [T, Hq]) where lse is True or a float32 tensor.  Rows of no
+        own among them; q_starts int32 [B + 1]: where each sequence's rows of q begin, max_q_len of them at most (rows beyond that are
+        not written; both None: row b is sequence b's only one).  Returns out [T, Hq, 128], or (out, lse [T, Hq]) where lse is True or a float32 tensor.  Rows of no
         sequence are left as they were (a new out has zeros there)."""
         t, at = q.shape[0], self._at
         b, each = page_table.shape

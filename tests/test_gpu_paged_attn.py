@@ -237,6 +237,23 @@ def test_pages_outside_the_cache_stand_for_zeros(bits):
 
 
 @BOTH
+def test_pages_outside_the_cache_with_many_sixteens(bits):
+    """Every sixteen of a page's tokens, not its first alone, and page 0, whose address stands in for that of none, holds numbers."""
+    page = 64
+    cache = tkv.PagedCache(n_q_heads=8, n_kv_heads=2, page_size=page, bits=bits, n_pages=6)
+    k, v = (torch.randn(6 * page, 2, 128, device="cuda").half() for _ in range(2))
+    slots = torch.arange(6 * page, device="cuda", dtype=torch.int32)
+    cache.append(None, k, v, slots)
+    k, v = (_f64(x) for x in cache.gather(slots))
+    table = torch.tensor([[1, 6, 2, -3, 0]], device="cuda", dtype=torch.int32)
+    kk, vv = (np.concatenate([x[p * page:(p + 1) * page] if 0 <= p < 6 else 0 * x[:page] for p in table[0].tolist()])[:300] for x in (k, v))
+    q = torch.randn(1, 8, 128, device="cuda").half()
+    out, lse = cache.attend(q, SM, table, torch.tensor([300], device="cuda", dtype=torch.int32), lse=True)
+    torch.cuda.synchronize()
+    _compare(out, lse, _f64(q), kk, vv, torch.float16)
+
+
+@BOTH
 def test_shared_pages(bits):
     """Sequences whose first pages are the same ones."""
     page = 16

@@ -4,6 +4,7 @@ import ctypes as C
 import os
 
 import pytest
+import torch
 
 import paper_2505_19586_amd as tkv
 from paper_2505_19586_amd import build as tkv_build
@@ -148,3 +149,22 @@ def test_null_descriptors(L):
 def test_axes_of_sections():
     assert tkv.rope_axes((2, 3, 1)) == bytes([0, 0, 1, 1, 1, 2])
     assert tkv.rope_axes((2, 3, 1), interleaved=True) == bytes([0, 1, 2, 0, 1, 1])
+    for interleaved in (False, True):
+        with pytest.raises(AssertionError):
+            tkv.rope_axes((2, -1, 3), interleaved)
+
+
+def test_tensors_of_the_host():
+    """Refused as what is wrong, also where there is no GPU."""
+    x = torch.zeros(2, 4, 128, dtype=torch.float16)
+    with pytest.raises(AssertionError):
+        tkv.qk_norm_rope(x, x, None, None)
+    with pytest.raises(AssertionError):
+        tkv.PagedCache(n_q_heads=4, n_kv_heads=4, page_size=16, k_pages=x.new_zeros(2, 4, 16, 128), v_pages=x.new_zeros(2, 4, 16, 128))
+
+
+def test_strides_whose_span_leaves_64_bits(L):
+    n = C.c_size_t()
+    wide = dict(n_pages=(1 << 27) - 1, page_size=16, n_kv_heads=8)
+    for strides, status in (((1 << 36, 1 << 33, 1 << 22), -1), ((1 << 33, 1 << 29, 1 << 22), 0)):
+        assert L.tkv_paged_cache_sizes(C.byref(_paged(**wide, k_stride=strides, v_stride=strides)), C.byref(n)) == status
