@@ -369,9 +369,10 @@ __device__ inline void weigh(Rows<NT>& r, floatx4 (&s)[NT][Y], uintx4 (&w)[NT][Y
 }
 
 // A place of 16 bytes in a row of LDS: rows of 256 bytes keep their sixteen places in an order that depends on the row, so that the reads
-// (a column of keys; a 4 x 16 block of values) and writes meet all banks.
+// (a column of keys; a 4 x 16 block of values) and writes meet all banks (no conflicts counted).  For values eight rows differ in a place's
+// upper three bits, for the reads of 32 bytes of a row, and in its lower three, for writes of 16.
 __device__ inline int k_place(int row, int place) { return place ^ (row & 15); }
-__device__ inline int v_place(int row, int place) { return place ^ (((row & 7) << 1) | ((row >> 3) & 1)); }
+__device__ inline int v_place(int row, int place) { return place ^ (((row & 7) << 1) | (((row >> 2) ^ (row >> 3)) & 1)); }
 // Where a lane's transposing read of the first sixteen channels of sixteen values begins (channels 16 ct on: 32 ct in its bits 5 to 7, exclusive or).
 __device__ inline int v_read_at() {
   const int lane = threadIdx.x % 64, col = lane % 16, row = 4 * (lane / 16) + col / 4;
