@@ -2,7 +2,7 @@
 // keys and values that lie in pages, in 16 bits or as microscaled 4-bit numbers, for single tokens, drafts and short chunks.
 //
 // The bytes of the cache bound the attention: 16 sequences of 16000 tokens, 8 KV heads, 16 bits (1.05 GB) 182 us, 5.8 TB/s; 4 of
-// 131072 in 4 bits (0.57 GB) 111 us, 5.1 TB/s (a read of 2 GiB alone reaches 5.4); short calls are a chain of round trips: one token over
+// 131072 in 4 bits (0.57 GB) 109 us, 5.2 TB/s (a read of 2 GiB alone reaches 5.4); short calls are a chain of round trips: one token over
 // 128 keys 5.6 us, over 512 8.0, 64 sequences of up to 300 19.
 //
 // The query heads of a KV head, of all the call's tokens of a sequence, are rows of one matrix, sixteen to an operand, so that keys and values
@@ -43,7 +43,8 @@ struct GatherParams {
 
 // Rows from pages, contiguous.  A wave takes 4 J tokens of one head's keys or values, sixteen lanes a row: neighbours in a page are read
 // side by side (64 bytes a row in 4 bits), and rows are written whole, past the caches' usual order (nontemporal: 20000 tokens of 16 bits
-// 30.6 -> 27.4 us, 100003 of 4 bits 118 -> 111; with 32 instead of 16 tokens a wave 111 -> 101.5).  Bound by the memory's rate.
+// 30.6 -> 27.4 us, 100003 of 4 bits 118 -> 111; with 32 instead of 16 tokens a wave 111 -> 101.5, 16 bits 27.6 -> 39).  Bound by the
+// memory's rate: 5.9 and 5.1 TB/s.
 template <typename T, int BITS, int J>
 __global__ __launch_bounds__(256) void paged_gather_kernel(GatherParams p) {
   const int lane = threadIdx.x % 64, sub = lane / 16, place = lane % 16;
@@ -473,7 +474,7 @@ struct Tiles16 {
 // products, which do not mind the order of the channels), keys from there to the matrix cores, values, as numbers of the type, 32 keys at a
 // time through LDS, whose reads transpose them.  The next tile's codes are sent for as soon as this one's have left their registers: eight
 // waves a unit with 8.5 KiB each on its way.  (Twelve, as registers would allow with 16 rows: 16 sequences of 100 to 2000 tokens 16.4 -> 14.8
-// us, but 4 of 131072 111 -> 117, their ranges being cut less evenly.)
+// us, but 4 of 131072 111 -> 117.  Two tiles ahead, in a second set of registers: 111 -> 126.)
 template <typename T, int NT>
 struct Tiles4 {
   static constexpr int kKeys = 64, kPer = 4, kBytes = 32 * TKV_D * 2;
@@ -589,8 +590,9 @@ __device__ inline void clear_rows_of_no_sequence() {
 
 // An item's parts: where a range's cut lies in it, its tiles are several waves', and their results (sum, reference, weighted sums) have to
 // be joined.  They are left in the workspace, a counter says who comes last, and that workgroup joins them: no second launch (3.4 us and
-// its way there: one token over 2048 keys 13.7 -> 9 us in all).  Nobody waits for anybody.  A workgroup whose whole range lies in one item joins its waves' results itself and has one part (slot 8 g); elsewhere
-// every wave has its own: slot 2 w for one that begins with the wave's range, 2 w + 1 otherwise.
+// its way there: one token over 2048 keys 13.7 -> 9 us in all).  Nobody waits for anybody.  A workgroup whose whole range lies in one item
+// joins its waves' results itself and has one part (slot 8 g); elsewhere every wave has its own: slot 2 w
+// for one that begins with the wave's range, 2 w + 1 otherwise.
 struct Parts {
   uint32_t start, pw;           // the item's first tile, tiles of a wave's range
   int32_t w0, g0, g1;           // first wave, first and last workgroup

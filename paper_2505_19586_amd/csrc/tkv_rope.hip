@@ -6,9 +6,14 @@
 //   a cos - b sin, b cos + a sin.
 //
 // Every element is read once and written once: the memory's rate bounds long prompts (32768 tokens of 48 heads: 136 us, 5.9 TB/s, half
-// of the input still in the last-level cache; a large copy reaches 5.1), the latency of one round trip a few tokens (16: 3.3 us).  Eight lanes take a row (a head of a token), sixteen channels each, chosen so
+// of the input still in the last-level cache; a large copy reaches 5.1), the latency of one round trip a few tokens (16: 3.3 us).  Eight
+// lanes take a row (a head of a token), sixteen channels each, chosen so
 // that both channels of every pair lie in one lane: nothing is exchanged but the row's sum of squares.  A token's
 // angles are worked out once per wave, one frequency per lane, and handed round.
+//
+// Several axes cost nothing: the axis of a lane's frequency is two bits of two masks (24640 tokens, three axes: 103 us, 5.9 TB/s).  Into pages
+// a row goes straight from its registers (12289 tokens, 16 bits: 54 us, 5.5 TB/s; 32 tokens: 3.9 us), in 4 bits by way of its blocks' largest
+// magnitudes, three exchanges over the row's eight lanes each (8191 tokens: 35 us, 5.1 TB/s).
 #include <type_traits>
 
 #include "tkv_common.h"

@@ -798,6 +798,7 @@ class PagedCache:
         self._pages = k_pages.data_ptr(), v_pages.data_ptr()
         self._desc_at = C.addressof(self.desc)
         self._rows = (n_q_heads, head_dim), (n_kv_heads, head_dim)
+        self._none = torch.empty(0, dtype=dtype, device=self.device)  # (its new_empty spares half a microsecond of torch.empty's two)
         self._workspaces = _Workspaces(self.workspace_bytes, torch.device("cuda", self._at), at_once=False, zeros=12288)  # (a cache that is only filled needs none)
 
     def _slots(self, slots, t):
@@ -836,16 +837,16 @@ class PagedCache:
         t = slots.shape[0]
         self._slots(slots, t)
         handle = _handle(self._at, stream)
-        outs = []
+        shape = t, *self._rows[1]
         for o in (k_out, v_out):
-            if o is None:
-                o = _new((t, *self._rows[1]), self.dtype, self.device, stream)
-            else:
-                assert o.dtype == self.dtype and o.shape == (t, *self._rows[1]) and o.is_contiguous() and o.get_device() == self._at
-            outs.append(o)
-        _check(lib().tkv_paged_gather(self._desc_at, *self._pages, t, slots.data_ptr(), outs[0].data_ptr(), outs[1].data_ptr(),
-                                      handle), "tkv_paged_gather")
-        return outs[0], outs[1]
+            assert o is None or (o.dtype == self.dtype and o.shape == shape and o.is_contiguous() and o.get_device() == self._at)
+        if k_out is None:
+            k_out = self._none.new_empty(shape) if stream is None else _new(shape, self.dtype, self.device, stream)
+        if v_out is None:
+            v_out = torch.empty_like(k_out) if stream is None else _new(shape, self.dtype, self.device, stream)
+        _check(lib().tkv_paged_gather(self._desc_at, *self._pages, t, slots.data_ptr(), k_out.data_ptr(), v_out.data_ptr(), handle),
+               "tkv_paged_gather")
+        return k_out, v_out
 
     def attend(self, q: torch.Tensor, sm_scale: float, page_table: torch.Tensor, k_lens: torch.Tensor, *,
                q_starts: torch.Tensor | None = None, max_q_len: int | None = None, out: torch.Tensor | None = None,
@@ -874,7 +875,10 @@ class PagedCache:
         else:
             assert out.dtype == q.dtype and out.shape == q.shape and out.is_contiguous() and out.get_device() == at
         if new_lse:
-            lse = _new(q.shape[:2], torch.float32, q.device, stream, -float("inf") if fill else None)
+            if stream is None and not fill:
+                lse = q.new_empty((t, self._rows[0][0]), dtype=torch.float32)
+            else:
+                lse = _new(q.shape[:2], torch.float32, q.device, stream, -float("inf") if fill else None)
         elif lse is False or lse is None:
             lse = None
         else:
