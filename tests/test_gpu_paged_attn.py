@@ -253,6 +253,23 @@ def test_pages_outside_the_cache_with_many_sixteens(bits):
     _compare(out, lse, _f64(q), kk, vv, torch.float16)
 
 
+def test_tables_without_pages():
+    cache = tkv.PagedCache(n_q_heads=4, n_kv_heads=2, n_pages=2)
+    q = torch.randn(3, 4, 128, device="cuda").half()
+    table = torch.empty(3, 0, device="cuda", dtype=torch.int32)
+    for n in (0, 5):
+        out, lse = cache.attend(q, SM, table, torch.full((3,), n, device="cuda", dtype=torch.int32), lse=True)
+        torch.cuda.synchronize()
+        assert not out.any() and torch.isneginf(lse).all()
+
+
+@BOTH
+@pytest.mark.parametrize("hq,hkv", [(1024, 1), (1024, 1024), (1000, 8)])
+def test_most_heads(hq, hkv, bits):
+    print(f"case heads {hq}/{hkv} {bits} bits", flush=True)
+    _run([1, 2], [65, 30], hq, hkv, 16, bits, seed=hkv)
+
+
 @BOTH
 def test_shared_pages(bits):
     """Sequences whose first pages are the same ones."""
