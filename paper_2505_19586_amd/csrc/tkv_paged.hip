@@ -509,6 +509,14 @@ struct Tiles4 {
       scales[y] = __builtin_amdgcn_raw_buffer_load_b8(from, at, scales_at + place * tkv::kScales4, 0);
     }
   }
+  // The next tile's codes go out before the other wave of the SIMD works on, and of the two that of the later workgroup, which otherwise
+  // comes second every time, comes first (16 sequences of 16000 tokens 62.7 -> 59.3 us, 4 of 131072 110 -> 106.4; without the latter 62, 109).
+  __device__ void ahead(const char* pages, const Plan<kPer>& plan, uint32_t tile, uintx4 (&codes)[4], uint32_t (&scales)[4]) {
+    __builtin_amdgcn_s_setprio(2);
+    fetch(pages, plan, tile, codes, scales);
+    if (2 * blockIdx.x >= gridDim.x) __builtin_amdgcn_s_setprio(1);
+    else __builtin_amdgcn_s_setprio(0);
+  }
   __device__ void begin(const Plan<kPer>& plan, uint32_t tile) {
     fetch(k_pages, plan, tile, k, ks);
     fetch(v_pages, plan, tile, v, vs);
@@ -533,7 +541,7 @@ struct Tiles4 {
       }
       if (z == 1 && more) {
         next();
-        fetch(k_pages, plan, tile, k, ks);
+        ahead(k_pages, plan, tile, k, ks);
       }
 #pragma unroll
       for (int y = 0; y < 2; ++y) {
@@ -553,7 +561,7 @@ struct Tiles4 {
       }
       __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
     }
-    if (more) fetch(v_pages, plan, tile, v, vs);
+    if (more) ahead(v_pages, plan, tile, v, vs);
   }
 };
 
