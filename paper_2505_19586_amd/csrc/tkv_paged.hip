@@ -916,7 +916,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void paged_attn_kernel(PagedParams)
     if (threadIdx.x == 0) __hip_atomic_store(p->arrivals + parts.w0, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
     const int rows = at.sq.q_len * walk.group - kRows * at.tile;
     const bool shared = rows <= 4 || (rows <= 8 && parts.count > 8);
-    const int team = shared ? (parts.count <= 4 && !together ? 1 : kWaves) : rows <= 8 ? 2 : kWaves;
+    const int team = shared ? (together || rows > 4 || parts.count > 8 ? kWaves : parts.count > 4 ? 2 : 1) : rows <= 8 ? 2 : kWaves;
     const int first = team == 1 ? next % kWaves : team == 2 ? (next + 1) & 2 : 0;
     next = first + team;
     const int mine = wave - first;
