@@ -548,3 +548,18 @@ def test_two_graphs_and_eager_calls_of_one_object():
         torch.cuda.synchronize()
         for got, w in zip((*outs, eager), want):
             assert torch.equal(got[0], w[0]) and torch.equal(got[1], w[1])
+
+
+@BOTH
+def test_parts_of_earlier_calls_do_not_matter_and_counters_end_at_zero(bits):
+    """The workspace's parts may hold anything before a call, NaN and infinities included; its counters are 0 after every one."""
+    lens = [3000, 700, 0, 20011, 33, 5000]
+    print(f"case poisoned workspace {bits} bits", flush=True)
+    cache, q, table, k_lens, want = _run([1] * 6, lens, 8, 2, 32, bits, seed=30, starts=False)
+    workspace = list(cache._workspaces._of.values())[0]
+    counters = workspace[-12288:]
+    for i in range(30):
+        workspace[:-12288].fill_((0xFF, 0x7C, 0x00)[i % 3])
+        out = cache.attend(q, SM, table, k_lens)
+        torch.cuda.synchronize()
+        assert torch.equal(out, want) and not counters.any(), i
