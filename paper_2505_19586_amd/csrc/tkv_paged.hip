@@ -91,9 +91,11 @@ __global__ __launch_bounds__(256) void paged_gather_kernel(GatherParams p) {
 
 constexpr int kWaves = 4;              // of a workgroup
 constexpr int kRowFloats = TKV_D + 4;  // of a row of partial sums in LDS (the four keep the banks apart)
-// Weights are 2^(logit - reference + kShift), and the reference follows a row's maximum only when that is 8 above it: at most 2^15, inside
-// fp16's range.
-constexpr float kShift = 7.f;
+// Weights are 2^(logit - reference + kShift), at most 2^kLargest, inside fp16's range: the reference follows a row's maximum only where a weight
+// is larger.  Whether one is, its exponent itself says, worked out as the weights are (one rounding): at logits of 2^26, in float32's steps
+// of 8, a maximum that is rounded by itself can be half a step too low.  kShift - reference is exact for the same reason: 8 is a
+// whole number of steps up to 2^27 in units of log 2 (logits of 2^26), 7 is one up to 2^24 only.
+constexpr float kShift = 8.f, kLargest = 15.f;
 constexpr float kNone = -3.402823466e38f;  // reference of a row without a key so far (finite: kNone - kNone is 0)
 constexpr int kMaxUnits = 256;             // compute units that the workspace has room for
 constexpr int kMostParts = 64;             // of an item (in workgroups), so that joining them stays short
@@ -347,9 +349,8 @@ __device__ inline void weigh(Rows<NT>& r, floatx4 (&s)[NT][Y], uintx4 (&w)[NT][Y
     for (int y = 0; y < Y; ++y)
 #pragma unroll
       for (int i = 0; i < 4; ++i) top = fmaxf(top, s[n][y][i]);
-    top *= scale2;
-    if (__builtin_expect(__builtin_amdgcn_ballot_w64(top > r.ref[n] + 8.f) != 0, 0)) {
-      top = tkv::over_rows(top, [](float a, float b) { return fmaxf(a, b); });
+    if (__builtin_expect(__builtin_amdgcn_ballot_w64(__builtin_fmaf(top, scale2, kShift - r.ref[n]) > kLargest) != 0, 0)) {
+      top = tkv::over_rows(top * scale2, [](float a, float b) { return fmaxf(a, b); });
       const float next = fmaxf(r.ref[n], top), shrink = __builtin_amdgcn_exp2f(r.ref[n] - next);
       r.ref[n] = next;
       r.sum[n] *= shrink;
