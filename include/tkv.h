@@ -615,7 +615,7 @@ int32_t tkv_paged_attn_sizes(const tkv_paged_desc* desc, size_t* workspace_bytes
  * q, out [n_tokens][Hq][128] contiguous; lse float32 [n_tokens][Hq] (natural logarithm of the sum of exponentials) or NULL.  Rows of out and
  * lse that belong to no sequence (in front of the first, behind the last) are left as they were, or with clear_rest = 1 get zeros and
  * -inf.  max_q_len: the most queries that a sequence has, as the host knows it; where q_starts say more, the first that many count
- * as all it has, and the others' rows are not written.
+ * as all it has, and the others' rows are of no sequence.
  * Limits (TKV_E_UNSUPPORTED beyond): pages_each * page_size <= 2^30, max_q_len * (Hq/Hkv) <= 2^24, max_q_len * (Hq/Hkv)^2 < 2^32, and
  * batch * Hkv * ceil(max_q_len * (Hq/Hkv) / 16) * (pages_each * page_size / 32 + 1) < 2^31 (max_q_len: n_tokens where that is less).
  * Keys behind a sequence's last are never used, whatever their slots hold; a non-finite value of a later token of the same call may still

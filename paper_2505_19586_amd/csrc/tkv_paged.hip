@@ -584,16 +584,21 @@ constexpr int lds_bytes() {
   return std::max(kWaves * Tiles<T, BITS, NT>::kBytes, kWaves * 16 * (kRowFloats + 2) * 4 + 16) + (int)sizeof(Won) * kWaves;
 }
 
-// Zeros, and -inf, for rows in front of the first sequence and behind the last.
+// Zeros, and -inf, for rows of no sequence: in front of the first, behind the last, and beyond the most that one may have.
 template <typename T>
 __device__ inline void clear_rows_of_no_sequence() {
   const Args p = arguments();
   const int front = min(max(p->q_starts[0], 0), p->n_tokens), back = min(max(p->q_starts[p->batch], front), p->n_tokens);
   const int none = front + p->n_tokens - back, row_places = p->hq * TKV_D / 8;
-  for (int i = blockIdx.x; i < none; i += gridDim.x) {
-    const int64_t token = i < front ? i : back + (i - front);
+  auto clear = [&](int64_t token) {
     for (int c = threadIdx.x; c < row_places; c += 64 * kWaves) ((uintx4*)p->out)[token * row_places + c] = (uintx4){0u, 0u, 0u, 0u};
     for (int c = threadIdx.x; p->lse && c < p->hq; c += 64 * kWaves) p->lse[token * p->hq + c] = -INFINITY;
+  };
+  for (int i = blockIdx.x; i < none; i += gridDim.x) clear(i < front ? i : back + (i - front));
+  for (int b = blockIdx.x; b < p->batch; b += gridDim.x) {
+    const int start = min(max(p->q_starts[b], 0), p->n_tokens), end = min(p->q_starts[b + 1], p->n_tokens);
+    if (__builtin_expect(end - start > p->max_q_len, 0))
+      for (int token = start + p->max_q_len; token < end; ++token) clear(token);
   }
 }
 

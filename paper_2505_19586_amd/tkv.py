@@ -853,8 +853,8 @@ class PagedCache:
                lse: bool | torch.Tensor = False, stream=None):
         """tkv_paged_attn: q [T, Hq, 128]; page_table int32 [B, pages], k_lens int32 [B]: each sequence's pages and tokens, the queries'
         own among them; q_starts int32 [B + 1]: where each sequence's rows of q begin, max_q_len of them at most (rows beyond that are
-        not written; both None: row b is sequence b's only one).  Returns out [T, Hq, 128], or (out, lse [T, Hq]) where lse is True or a float32 tensor.  Rows of no
-        sequence are left as they were (a new out has zeros there)."""
+        of no sequence; both None: row b is sequence b's only one).  Returns out [T, Hq, 128], or (out, lse [T, Hq]) where lse is True or a
+        float32 tensor.  Rows of no sequence are left as they were (new outputs have zeros there, and -inf)."""
         t, at = q.shape[0], self._at
         b, each = page_table.shape
         assert q.dtype == self.dtype and q.shape[1:] == self._rows[0] and q.is_contiguous() and q.get_device() == at

@@ -1,0 +1,35 @@
+"""tkv_paged_attn: rows of outputs that nobody attends for."""
+import pytest
+import torch
+
+import paper_2505_19586_amd as tkv
+
+pytestmark = pytest.mark.gpu
+SM = 128 ** -0.5
+
+
+@pytest.mark.parametrize("batch", [2, 700])
+def test_rows_beyond_the_most_that_a_sequence_may_have_are_of_none(batch):
+    """New outputs hold zeros and -inf there, given ones what they held; more sequences than workgroups."""
+    print(f"case rows beyond max_q_len, {batch} sequences", flush=True)
+    cache = tkv.PagedCache(n_q_heads=4, n_kv_heads=2, n_pages=1)
+    cache.v_pages[0, :, :5] = 3
+    q = torch.randn(6 * batch, 4, 128, device="cuda").half()
+    starts = 6 * torch.arange(batch + 1, device="cuda", dtype=torch.int32)
+    table, lens = torch.zeros(batch, 1, device="cuda", dtype=torch.int32), torch.full((batch,), 5, device="cuda", dtype=torch.int32)
+
+    def rows(x):
+        x = x.view(batch, 6, *x.shape[1:])
+        return x[:, :2], x[:, 2:]
+
+    junk = [torch.full(s, float("nan"), dtype=d, device="cuda") for s, d in ((q.shape, torch.float16), ((6 * batch, 4), torch.float32))]
+    del junk                                                              # (what a new tensor's memory may hold)
+    out, lse = cache.attend(q, SM, table, lens, q_starts=starts, max_q_len=2, lse=True)
+    torch.cuda.synchronize()
+    (have, rest), (lse_have, lse_rest) = rows(out), rows(lse)
+    assert (have == 3).all() and not rest.any() and lse_have.isfinite().all() and torch.isneginf(lse_rest).all()
+    out, lse = torch.full_like(q, 7.0), torch.full((6 * batch, 4), 5.0, device="cuda")
+    cache.attend(q, SM, table, lens, q_starts=starts, max_q_len=2, out=out, lse=lse)
+    torch.cuda.synchronize()
+    (have, rest), (_, lse_rest) = rows(out), rows(lse)
+    assert (have == 3).all() and (rest == 7).all() and (lse_rest == 5).all()
