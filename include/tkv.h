@@ -611,7 +611,7 @@ int32_t tkv_paged_attn_sizes(const tkv_paged_desc* desc, size_t* workspace_bytes
  * [batch]), token t of them at place t % page_size of page page_table[b][t / page_size] (device int32 [batch][pages_each]; entries behind
  * the last token are not read), and its queries are its newest tokens: rows q_starts[b] to q_starts[b + 1] - 1 of q and out (device int32
  * [batch + 1], ascending; NULL: row b alone, n_tokens = batch).  Token i of n queries sees keys j <= i + k_lens[b] - n.
- * out = softmax(sm_scale q.k) v; a token that sees no key yields zeros, and -inf in lse.
+ * out = softmax(sm_scale q.k) v; a token that sees no key yields zeros, and -inf in lse (one whose every logit is -inf: NaN, and -inf).
  * q, out [n_tokens][Hq][128] contiguous; lse float32 [n_tokens][Hq] (natural logarithm of the sum of exponentials) or NULL.  Rows of out and
  * lse that belong to no sequence (in front of the first, behind the last) are left as they were, or with clear_rest = 1 get zeros and
  * -inf.  max_q_len: the most queries that a sequence has, as the host knows it; where q_starts say more, the first that many count

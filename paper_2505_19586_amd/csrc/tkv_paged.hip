@@ -666,7 +666,7 @@ __device__ inline int64_t row_out(Args p, const Place& x, int row) {
   return (int64_t)(x.sq.q_start + token) * p->hq + x.h * group + head;
 }
 __device__ inline float log_sum(float ref, float sum) {
-  return sum == 0.f ? -INFINITY : (ref - kShift + __builtin_amdgcn_logf(sum)) * 0.69314718055994531f;
+  return ref == kNone ? -INFINITY : (ref - kShift + __builtin_amdgcn_logf(sum)) * 0.69314718055994531f;
 }
 
 // A wave joins an item's parts for some of its rows, a lane eight channels: row0, row0 + step, ..., each row's parts shared out over the
@@ -723,7 +723,7 @@ __device__ inline void join_rows(Args p, const Place& x, const Parts& parts, int
       }
       if (share == 0 && row + sub < rows) {
         const int64_t to = row_out(p, x, ROWS * x.tile + row + sub);
-        *(uintx4*)((T*)p->out + to * TKV_D + c) = pack8<T>(acc * (l == 0.f ? 0.f : 1.f / l));  // (no key: zeros)
+        *(uintx4*)((T*)p->out + to * TKV_D + c) = pack8<T>(acc * (1.f / l));
         if (p->lse && c == 0) p->lse[to] = log_sum(m, l);
       }
       m = kNone;
@@ -779,7 +779,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void paged_attn_kernel(PagedParams)
       const int row = min(at.tile * kRows + 16 * m + col, rows - 1);
       r.limit[m] = row_token(p, row) + ahead;
       r.ref[m] = kNone;
-      r.sum[m] = 0.f;
+      r.sum[m] = r.limit[m] < 0 ? 1.f : 0.f;  // (no key: 0 / 1, zeros; logits of -inf alone: 0 / 0)
 #pragma unroll
       for (int ct = 0; ct < 8; ++ct) r.o[m][ct] = (floatx4){0.f, 0.f, 0.f, 0.f};
     }
@@ -833,7 +833,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void paged_attn_kernel(PagedParams)
         if (parts.count == 1) {
           typedef T T4 __attribute__((ext_vector_type(4)));
           const int64_t to = row_out(p, done, row);
-          const float inv = sum == 0.f ? 0.f : 1.f / sum;  // (no key: zeros)
+          const float inv = 1.f / sum;
 #pragma unroll
           for (int ct = 0; ct < 8; ++ct) *(T4*)((T*)p->out + to * TKV_D + 16 * ct + 4 * quarter) = __builtin_convertvector(r.o[m][ct] * inv, T4);
           if (p->lse && quarter == 0) p->lse[to] = log_sum(r.ref[m], sum);
@@ -887,7 +887,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void paged_attn_kernel(PagedParams)
           continue;
         }
         const int64_t to = row_out(p, done, row);
-        *(uintx4*)((T*)p->out + to * TKV_D + c) = pack8<T>(acc * (sum == 0.f ? 0.f : 1.f / sum));  // (no key: zeros)
+        *(uintx4*)((T*)p->out + to * TKV_D + c) = pack8<T>(acc * (1.f / sum));
         if (p->lse && c == 0) p->lse[to] = log_sum(top, sum);
       }
       if (parts.count > 1) {

@@ -96,3 +96,32 @@ def test_a_later_key_just_above_a_far_reference(far):
     for b in range(0, batch, 100):
         _compare(out[b:b + 1], lse[b:b + 1], _f64(q[b:b + 1]), _f64(k), _f64(v), torch.float16, sm)
     assert (out == out[0]).all()
+
+
+@pytest.mark.parametrize("dtype", [torch.float16, torch.bfloat16])
+@pytest.mark.parametrize("batch,nq,n", [(1, 1, 5), (1, 1, 9000), (300, 1, 400), (40, 7, 3), (2, 5, 3000)])
+def test_logits_of_minus_infinity(batch, nq, n, dtype):
+    """Rows whose every key has a logit of -infinity: 0 / 0, not the zeros of rows without keys; with one finite logit among them, its
+    key's value."""
+    print(f"case {batch} times {nq} over {n} {dtype}, logits of -inf", flush=True)
+    page = 64
+    each = -(-n // page)
+    cache = tkv.PagedCache(n_q_heads=8, n_kv_heads=2, page_size=page, dtype=dtype, n_pages=each)
+    k = torch.ones(n, 2, 128, device="cuda", dtype=dtype)
+    k[:, :, 7] = -float("inf")
+    k[n // 2, 1, 7] = 2                                   # (the second head's)
+    v = torch.randn(n, 2, 128, generator=torch.Generator(device="cuda").manual_seed(n), device="cuda").to(dtype)
+    cache.append(None, k, v, torch.arange(n, device="cuda", dtype=torch.int32))
+    q = torch.ones(batch * nq, 8, 128, device="cuda", dtype=dtype)
+    table = torch.arange(each, device="cuda", dtype=torch.int32).repeat(batch, 1)
+    lens = torch.full((batch,), n, device="cuda", dtype=torch.int32)
+    starts = nq * torch.arange(batch + 1, device="cuda", dtype=torch.int32)
+    out, lse = cache.attend(q, 128 ** -0.5, table, lens, q_starts=starts, max_q_len=nq, lse=True)
+    torch.cuda.synchronize()
+    out, lse = out.view(batch, nq, 2, 4, 128), lse.view(batch, nq, 2, 4)
+    last = torch.arange(nq, device="cuda") + n - nq       # last key that a query sees
+    seen, one = last >= 0, last >= n // 2
+    assert not out[:, ~seen].any() and torch.isneginf(lse[:, ~seen]).all()
+    assert out[:, seen, 0].isnan().all() and torch.isneginf(lse[:, seen, 0]).all()
+    assert out[:, seen & ~one, 1].isnan().all()
+    assert (out[:, one, 1] == v[n // 2, 1]).all() and lse[:, one, 1].isfinite().all()
