@@ -304,12 +304,19 @@ __device__ inline void lds_write16(lds_char* at, uintx4 x) { *(__attribute__((ad
 __device__ inline uintx2 lds_read_tr(lds_char* at) {
   return __builtin_bit_cast(uintx2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) shortx4*)at));
 }
-// 16 bytes per lane from a descriptor's array straight to LDS, in lane order from `to` (uniform) on.  By hand, because the compiler
-// lets every transposing LDS read wait for all such loads, those of the next tile too; nothing lands in registers, and the caller
-// waits itself (vmcnt) before anyone reads the buffer.  (m0 is used by nothing else here: the compiler, which
-// cannot be told of it, since it is reserved, never does; tests/test_lds_loads_m0.py looks.)
-__device__ inline void to_lds(__amdgpu_buffer_rsrc_t from, uint32_t to, uint32_t lane_offset) {
-  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(to), "v"(lane_offset), "s"(from) : "memory");
+// Four times 16 bytes per lane from a descriptor's array straight to LDS, 1 KiB each, in lane order from `to` (uniform) on.  By hand,
+// because the compiler lets every transposing LDS read wait for all such loads, those of the next tile too; nothing lands in registers, and
+// the caller waits itself (vmcnt) before anyone reads the buffer.  (m0 is used by nothing else here: the compiler, which
+// cannot be told of it, since it is reserved, never does; and it does not know that a descriptor that the vector unit has just
+// written, by readfirstlane, is there for a load five wait states later: the first two instructions.  tests/test_lds_loads.py looks for both.)
+__device__ inline void to_lds(__amdgpu_buffer_rsrc_t from, uint32_t to, const uint32_t (&lane_offset)[4]) {
+  asm volatile(
+      "s_mov_b32 m0, %0\n\ts_nop 3\n\tbuffer_load_dwordx4 %2, %1, 0 offen lds\n\t"
+      "s_add_u32 m0, m0, 0x400\n\ts_nop 0\n\tbuffer_load_dwordx4 %3, %1, 0 offen lds\n\t"
+      "s_add_u32 m0, m0, 0x400\n\ts_nop 0\n\tbuffer_load_dwordx4 %4, %1, 0 offen lds\n\t"
+      "s_add_u32 m0, m0, 0x400\n\ts_nop 0\n\tbuffer_load_dwordx4 %5, %1, 0 offen lds" ::"s"(to), "s"(from), "v"(lane_offset[0]),
+      "v"(lane_offset[1]), "v"(lane_offset[2]), "v"(lane_offset[3])
+      : "memory", "scc");
 }
 
 // A descriptor of `bytes` bytes from an address that is the same for all lanes, as the assembly above wants it: in scalar registers.
@@ -426,10 +433,8 @@ struct Tiles16 {
       const auto kr = uniform_array(k + of_lane(plan.k_at, l), rows == 0 ? 0 : (rows - 1) * k_st + TKV_D * 2);
       const auto vr = uniform_array(v + of_lane(plan.v_at, l), rows == 0 ? 0 : (rows - 1) * v_st + TKV_D * 2);
       const uint32_t to = to0 + 4096u * (uint32_t)y;
-#pragma unroll
-      for (int j = 0; j < 4; ++j) to_lds(kr, to + 1024 * j, k_off[j]);
-#pragma unroll
-      for (int j = 0; j < 4; ++j) to_lds(vr, to + kTile + 1024 * j, v_off[j]);
+      to_lds(kr, to, k_off);
+      to_lds(vr, to + kTile, v_off);
     }
   }
   __device__ void begin(const Plan<kPer>& plan, uint32_t tile) { stage(plan, tile, 0); }

@@ -101,7 +101,7 @@ __device__ inline uintx2 lds_read_tr(lds_char* at) {
 // 16 bytes per lane from a descriptor's array straight to LDS, in lane order from `to` (uniform) on.  By hand, because the
 // compiler lets every transposing LDS read wait for all such loads, those of the next tile's buffer too; nothing lands in
 // registers, and the caller waits itself (vmcnt) before anyone reads the buffer.  (m0 is used by nothing else here: the compiler, which
-// cannot be told of it, since it is reserved, never does; tests/test_lds_loads_m0.py looks.)
+// cannot be told of it, since it is reserved, never does; tests/test_lds_loads.py looks.)
 __device__ inline void to_lds(__amdgpu_buffer_rsrc_t from, uint32_t to, uint32_t lane_offset) {
   asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(to), "v"(lane_offset), "s"(from) : "memory");
 }

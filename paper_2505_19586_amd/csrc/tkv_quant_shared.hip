@@ -110,7 +110,7 @@ __device__ inline uintx2 lds_read_tr(lds_at at) {
 }
 // 16 bytes per lane straight to LDS, in lane order from `to` (uniform) on; the caller waits (vmcnt).  By hand, so that the compiler
 // makes no LDS read wait for loads of other slots.  (m0 is used by nothing else here: the compiler, which
-// cannot be told of it, since it is reserved, never does; tests/test_lds_loads_m0.py looks.)
+// cannot be told of it, since it is reserved, never does; tests/test_lds_loads.py looks.)
 __device__ inline void to_lds(const char* base, uint32_t lane_offset, uint32_t to) {
   asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(to), "v"(lane_offset), "s"(base) : "memory");
 }
