@@ -455,8 +455,12 @@ __global__ __launch_bounds__(64 * kFewWaves, 1) void prompt_few_kernel(PromptPar
     float top = s[0];
 #pragma unroll
     for (int i = 1; i < 16; ++i) top = fmaxf(top, s[i]);
-    top = fmaxf(top, other_half(top, half)) * p.scale2;
-    if (__builtin_amdgcn_ballot_w64(top > ref + 8.f) != 0) {
+    top = fmaxf(top, other_half(top, half));
+    // (The second: with logits of 2^23 and more float32's steps are 1 to 8, and `top`, rounded by itself, can be below what the weights'
+    // own exponents, rounded once, come to.  2^15.5 is inside fp16's range.)
+    const bool rises = top * p.scale2 > ref + 8.f || __builtin_fmaf(top, p.scale2, kShift - ref) > 15.5f;
+    if (__builtin_amdgcn_ballot_w64(rises) != 0) {
+      top *= p.scale2;
       const float next = fmaxf(ref, top), shrink = __builtin_amdgcn_exp2f(ref - next);
       ref = next;
       sum *= shrink;
