@@ -237,22 +237,25 @@ __device__ __attribute__((always_inline)) inline void attend(const SharedParams&
   }
   // logits s, to which base[t] is to be added, to weights; Sum: the rounded weights are added up here, not by the operand's row of ones
   auto soften = [&](floatx4 (&s)[2][NQ], const float (&base)[NQ], uintx4 (&w)[NQ], auto Sum) {
-    float rise = -INFINITY;
-    float top[NQ];
+    // (Whether a weight is too large, its exponent itself says, rounded once as it will be: with logits of 2^23 and more float32's steps
+    // are 1 to 8, and a maximum rounded by itself can be below what the exponents come to.)
+    float largest = -INFINITY;
+    float top[NQ], less[NQ];
 #pragma unroll
     for (int t = 0; t < NQ; ++t) {
       top[t] = s[0][t][0];
 #pragma unroll
       for (int i = 1; i < 8; ++i) top[t] = fmaxf(top[t], s[i / 4][t][i % 4]);
-      top[t] = __builtin_fmaf(top[t], p.scale2, base[t]);
-      rise = fmaxf(rise, top[t] - ref[t]);
+      less[t] = base[t] + kShift - ref[t];
+      largest = fmaxf(largest, __builtin_fmaf(top[t], p.scale2, less[t]));
     }
-    if (__builtin_amdgcn_ballot_w64(rise > kLazy) != 0) {
+    if (__builtin_amdgcn_ballot_w64(largest > kLazy + kShift) != 0) {
 #pragma unroll
       for (int t = 0; t < NQ; ++t) {
-        const float next = fmaxf(ref[t], tkv::over_rows(top[t], tkv::MaxOf{}));
+        const float next = fmaxf(ref[t], tkv::over_rows(__builtin_fmaf(top[t], p.scale2, base[t]), tkv::MaxOf{}));
         const float shrink = __builtin_amdgcn_exp2f(ref[t] - next);
         ref[t] = next;
+        less[t] = base[t] + kShift - next;
         sum[t] *= shrink;
 #pragma unroll
         for (int x = 0; x < 8; ++x) o[t][x] *= shrink;
@@ -261,11 +264,10 @@ __device__ __attribute__((always_inline)) inline void attend(const SharedParams&
     }
 #pragma unroll
     for (int t = 0; t < NQ; ++t) {
-      const float less = base[t] + kShift - ref[t];
       half8 v;
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
-        const float e = __builtin_amdgcn_exp2f(__builtin_fmaf(s[i / 4][t][i % 4], p.scale2, less));
+        const float e = __builtin_amdgcn_exp2f(__builtin_fmaf(s[i / 4][t][i % 4], p.scale2, less[t]));
         v[i] = (_Float16)e;
         if constexpr (decltype(Sum)::value) sum[t] += (float)v[i];
       }
