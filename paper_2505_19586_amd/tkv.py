@@ -866,6 +866,7 @@ class PagedCache:
             max_q_len = 1
         else:
             assert max_q_len is not None, "max_q_len: the most queries of a sequence"
+            max_q_len = min(int(max_q_len), max(t, 1))  # (a number beyond 32 bits would be another)
             assert q_starts.dtype == torch.int32 and q_starts.shape == (b + 1,) and q_starts.is_contiguous() and q_starts.get_device() == at
         new_lse = lse is True
         clear = q_starts is not None and out is None and (new_lse or not isinstance(lse, torch.Tensor))  # (by the call itself)
@@ -885,7 +886,7 @@ class PagedCache:
             assert lse.dtype == torch.float32 and lse.shape == q.shape[:2] and lse.is_contiguous() and lse.get_device() == at
         with self._workspaces.lock:
             workspace = self._workspaces.of(handle, stream)
-            status = lib().tkv_paged_attn(self._desc_at, *self._pages, b, t, int(max_q_len), q.data_ptr(), out.data_ptr(), _ptr(lse),
+            status = lib().tkv_paged_attn(self._desc_at, *self._pages, b, t, max_q_len, q.data_ptr(), out.data_ptr(), _ptr(lse),
                                           page_table.data_ptr(), each, k_lens.data_ptr(), _ptr(q_starts), clear, float(sm_scale),
                                           workspace.data_ptr(), self.workspace_bytes, handle)
         _check(status, "tkv_paged_attn")

@@ -33,3 +33,19 @@ def test_rows_beyond_the_most_that_a_sequence_may_have_are_of_none(batch):
     torch.cuda.synchronize()
     (have, rest), (_, lse_rest) = rows(out), rows(lse)
     assert (have == 3).all() and (rest == 7).all() and (lse_rest == 5).all()
+
+
+@pytest.mark.parametrize("most", [7, 2**31 - 1, 2**31, 2**32 + 1, 2**63 - 1, 2**64 + 2])
+def test_any_bound_on_queries(most):
+    """Numbers beyond 32 bits too."""
+    print(f"case max_q_len {most}", flush=True)
+    cache = tkv.PagedCache(n_q_heads=4, n_kv_heads=2, n_pages=1)
+    for x in (cache.k_pages, cache.v_pages):
+        x.normal_(generator=torch.Generator(device="cuda").manual_seed(0))
+    q = torch.randn(9, 4, 128, device="cuda").half()
+    starts = torch.tensor([0, 2, 9], device="cuda", dtype=torch.int32)
+    table, lens = torch.zeros(2, 1, device="cuda", dtype=torch.int32), torch.tensor([5, 60], device="cuda", dtype=torch.int32)
+    got = cache.attend(q, SM, table, lens, q_starts=starts, max_q_len=most)
+    want = cache.attend(q, SM, table, lens, q_starts=starts, max_q_len=7)
+    torch.cuda.synchronize()
+    assert torch.equal(got, want) and want.any(2).all()
