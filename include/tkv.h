@@ -625,8 +625,10 @@ int32_t tkv_paged_attn_sizes(const tkv_paged_desc* desc, size_t* workspace_bytes
  * 0 < sm_scale <= 2.3e38; logits (sm_scale q.k) of magnitude up to 2^26 are safe.  The result is the same bit for bit from call to call
  * (on streams that may use as many compute units).  Addresses of pages, q, out and workspace are multiples of 16 bytes; out and lse
  * must not overlap the inputs; concurrent calls need separate workspaces.
- * Up to about 64 tokens of a sequence this is the shorter way (64 tokens of 32/8 heads over 2000 in 16 bits 32 us, over 65536 in 4 bits 132);
- * for more, tkv_paged_gather and tkv_prompt_attn (333 over 65536 in 16 bits 508 us, against 1083).
+ * Rows of a sequence and KV head (tokens times Hq/Hkv) are taken 48 at a time (4 bits: 32), and its keys are read once for each of these:
+ * up to about 130 rows (4 bits: 400) this is the shorter way; for more, tkv_paged_gather and tkv_prompt_attn are, the more so the longer
+ * the cache (32/8 heads, us, this / those: 16 bits, 32 tokens over 8192 38 / 34, over 65536 137 / 166, 64 tokens over 2000 29 / 32, over
+ * 65536 248 / 179; 4 bits, 64 tokens over 65536 118 / 148, 128 210 / 207, 333 509 / 423).
  */
 int32_t tkv_paged_attn(const tkv_paged_desc* desc, const void* k_pages, const void* v_pages, int32_t batch, int32_t n_tokens,
                        int32_t max_q_len, const void* q, void* out, float* lse, const int32_t* page_table, int32_t pages_each,

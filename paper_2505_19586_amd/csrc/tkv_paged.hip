@@ -6,7 +6,7 @@
 // 128 keys 5.6 us, over 512 8.0, 64 sequences of up to 300 17.
 //
 // The query heads of a KV head, of all the call's tokens of a sequence, are rows of one matrix, sixteen to an operand, so that keys and values
-// are read once for all of them.  Both products are transposed (S^T = K Q^T, O^T = V^T P^T): a lane's column is a row of queries, its
+// are read once for up to 48 of them (4 bits: 32); of more rows every 48 (32) read them again.  Both products are transposed (S^T = K Q^T, O^T = V^T P^T): a lane's column is a row of queries, its
 // softmax statistics one number a lane, and its weights lie where the second product wants them: the keys of a lane's eight weights are 16 y
 // + 4 (lane / 16) + i, and the values' LDS reads, which transpose 4 x 16 elements on the way, take them in that order (a sum over keys does
 // not mind it).  One pass over the keys: running reference and sum in float32, weights rounded to the type for the second product (off by
@@ -93,8 +93,9 @@ constexpr int kWaves = 4;              // of a workgroup
 constexpr int kRowFloats = TKV_D + 4;  // of a row of partial sums in LDS (the four keep the banks apart)
 // Weights are 2^(logit - reference + kShift), at most 2^kLargest, inside fp16's range: the reference follows a row's maximum only where a weight
 // is larger.  Whether one is, its exponent itself says, worked out as the weights are (one rounding): at logits of 2^26, in float32's steps
-// of 8, a maximum that is rounded by itself can be half a step too low.  kShift - reference is exact for the same reason: 8 is a
-// whole number of steps up to 2^27 in units of log 2 (logits of 2^26), 7 is one up to 2^24 only.
+// of 8, a maximum that is rounded by itself can be half a step too low.  kShift is 8 for the same reason: a whole number of
+// steps up to 2^27 in units of log 2 (logits of 2^26), so that all references are less by the same (7 is one up to 2^24 only, and weights
+// under different references were up to 4 times too large beyond); next to a power of two the difference may be rounded by half a step.
 constexpr float kShift = 8.f, kLargest = 15.f;
 constexpr float kNone = -3.402823466e38f;  // reference of a row without a key so far (finite: kNone - kNone is 0)
 constexpr int kMaxUnits = 256;             // compute units that the workspace has room for
