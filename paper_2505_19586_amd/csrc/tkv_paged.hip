@@ -182,7 +182,7 @@ struct Walk {
       q_len = 1;
       if (starts) {
         q_start = min(max(starts[b], 0), p->n_tokens);
-        q_len = max(0, min(min(starts[b + 1], p->n_tokens) - q_start, p->max_q_len));
+        q_len = max(0, min(min(max(starts[b + 1], 0), p->n_tokens) - q_start, p->max_q_len));
       }
     }
     count = (uint32_t)(key_tiles(k_len) * row_tiles(q_len)) * (uint32_t)p->pages.hkv;  // (no rows: 0)
@@ -603,7 +603,7 @@ __device__ inline void clear_rows_of_no_sequence() {
   };
   for (int i = blockIdx.x; i < none; i += gridDim.x) clear(i < front ? i : back + (i - front));
   for (int b = blockIdx.x; b < p->batch; b += gridDim.x) {
-    const int start = min(max(p->q_starts[b], 0), p->n_tokens), end = min(p->q_starts[b + 1], p->n_tokens);
+    const int start = min(max(p->q_starts[b], 0), p->n_tokens), end = min(max(p->q_starts[b + 1], 0), p->n_tokens);
     if (__builtin_expect(end - start > p->max_q_len, 0))
       for (int token = start + p->max_q_len; token < end; ++token) clear(token);
   }

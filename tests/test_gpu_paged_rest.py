@@ -49,3 +49,23 @@ def test_any_bound_on_queries(most):
     want = cache.attend(q, SM, table, lens, q_starts=starts, max_q_len=7)
     torch.cuda.synchronize()
     assert torch.equal(got, want) and want.any(2).all()
+
+
+@pytest.mark.parametrize("low", [-2**31, -2**31 + 1, -2**31 + 40, -1])
+def test_starts_far_below_zero_reach_nothing(low):
+    """Invalid, but nothing out of bounds is touched: where one sequence would end below zero it has no rows, however far below."""
+    print(f"case starts with {low}", flush=True)
+    cache = tkv.PagedCache(n_q_heads=4, n_kv_heads=2, n_pages=1)
+    cache.v_pages[0, :, :5] = 3
+    q = torch.randn(5, 4, 128, device="cuda").half()
+    table, lens = torch.zeros(5, 1, device="cuda", dtype=torch.int32), torch.full((5,), 5, device="cuda", dtype=torch.int32)
+    whole, whole_lse = torch.full((64, 4, 128), 7.0, device="cuda").half(), torch.full((64, 4), 5.0, device="cuda")
+    for at in range(1, 6):                                # (the sequence in front of it would end there)
+        starts = torch.arange(6, device="cuda", dtype=torch.int32)
+        starts[at] = low
+        cache.attend(q, SM, table, lens, q_starts=starts, max_q_len=3, out=whole[:5], lse=whole_lse[:5])
+        cache.attend(q, SM, table, lens, q_starts=starts, max_q_len=3)
+        torch.cuda.synchronize()
+        assert (whole[5:] == 7).all() and (whole_lse[5:] == 5).all(), at
+        rows = [b for b in range(5) if b != at - 1 and b != at]
+        assert (whole[rows] == 3).all(), at
